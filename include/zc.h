@@ -303,6 +303,73 @@ int zc_reduce_step_part(const void* d_chunk, size_t chunk_bytes, const float* d_
 int zc_quality(const float* d_ref, const float* d_test, size_t n, double* out4,
                void* d_ws, size_t ws_bytes, void* hip_stream);
 
+/* ---- The calls around the collective: the optimiser's step that takes the averaged gradients, and layers in 4-bit blocks.
+ *
+ * All of them are asynchronous on hip_stream and return ZC_OK, ZC_ERR_ARG (nothing is launched then) or ZC_ERR_HIP; there is
+ * nothing to finish.  They can be captured into a HIP graph.  Buffers need the alignment of their own type only, unless said
+ * otherwise.  Sizes of zero are fine. */
+#define ZC_F32 0
+#define ZC_BF16 1
+#define ZC_F16 2
+
+/* One AdamW step over k tensors of n[i] values (any count; host arrays of k entries), in as few launches as their table allows
+ * (one for every 80 tensors).  For every value, in binary32, each operation rounded:
+ *   g = grad x *d_grad_scale;  m' = beta1 m + (1 - beta1) g;  v' = beta2 v + ((1 - beta2) g) g;  r = sqrt(v')
+ *   p' = p (1 - lr weight_decay) - (m' / (r / sqrt(1 - beta2^step) + eps)) (lr / (1 - beta1^step))
+ * d_params: updated in place; d_grads: read; param_type, grad_type: ZC_F32, ZC_BF16 or ZC_F16.  d_copies (may be NULL, as may its
+ * entries): p' is stored here too, as copy_type, for weights in fp32 that a program computes with in 16 bits.
+ * d_grad_scale (device, may be NULL): one binary32 factor of all gradients (a clip or an unscaling).  If it is not finite the call
+ * changes nothing.
+ * d_state: zc_adamw_state_bytes(n, k, state_bits) bytes, 16-byte aligned, zeros before the first step; it belongs to these tensors in this order.
+ * Tensor i has ceil(n[i] / 32) blocks of 32 values in it, behind those of the tensors before it; with B blocks in all:
+ *   state_bits 32: m, 32 B binary32 values | v, 32 B values
+ *   state_bits  8: m, 32 B codes | sqrt(v), 32 B codes | scale bytes of m, B, zero padded to a multiple of 16 | of sqrt(v), likewise
+ * A code is e4m3, a scale byte s stands for 2^(s - 127), 255 for a block with a value that is not finite (all NaN).  s is the exponent field
+ * of the block's largest magnitude minus 7, at least 0.  Codes are rounded to the nearest (ties to even) if seed is 0, otherwise up or
+ * down at random in proportion, which keeps small changes alive on average: value j of the state goes up when its 16 random bits
+ * over 65536 reach the way that is left.  The bits are hashed from seed, step and j, so that equal calls give equal results.
+ * A root that is not zero never gets the code of zero.
+ * step counts from 1.  Errors: ARG (also betas outside [0, 1), negative or not finite lr, eps, weight_decay, step 0, state too small), HIP. */
+size_t zc_adamw_state_bytes(const size_t* n, int k, int state_bits);
+int zc_adamw(int k, const size_t* n, void* const* d_params, int param_type, const void* const* d_grads, int grad_type,
+             void* const* d_copies, int copy_type, void* d_state, size_t state_bytes, int state_bits, uint64_t step, double lr, double beta1,
+             double beta2, double eps, double weight_decay, const float* d_grad_scale, uint64_t seed, void* hip_stream);
+
+/* Matrices in 4-bit blocks.  A row of cols values is held as ceil(cols / 32) blocks of 32 values: 16 bytes of codes (two a byte,
+ * the first one in the low bits), and a scale byte.  A code is e2m1 (sign, then 0 0.5 1 1.5 2 3 4 6), a scale byte s stands for
+ * 2^(s - 127), 255 for a block with a value that is not finite (32 NaNs, codes 0).  s is the exponent field of the block's largest magnitude
+ * minus 2, at least 0; codes are rounded to the nearest, ties to even, and at most 6.  The last block of a row is filled up with zeros.
+ * Codes: rows codes_stride bytes apart, a multiple of 16, 16-byte aligned.  Scale bytes: rows scales_stride bytes
+ * apart, a multiple of 4, 4-byte aligned.  The smallest strides: */
+size_t zc_mx_codes_stride(size_t cols);
+size_t zc_mx_scales_stride(size_t cols);
+
+/* rows x cols values (type; rows `stride` values apart) into blocks along the rows (d_codes, d_scales), into the blocks of
+ * the transposed matrix, cols x rows, whose blocks run down the columns of d_in (d_codes_t, d_scales_t), or both in one pass: pointers of
+ * the one that is not wanted are NULL.  A layer's output gradient needs both, for the gradients of its input and of its weights. */
+int zc_mx_quantize(const void* d_in, int type, size_t rows, size_t cols, size_t stride, void* d_codes, size_t codes_stride, void* d_scales,
+                   size_t scales_stride, void* d_codes_t, size_t codes_t_stride, void* d_scales_t, size_t scales_t_stride, void* hip_stream);
+
+/* What blocks stand for, rounded to type. */
+int zc_mx_dequantize(const void* d_codes, size_t codes_stride, const void* d_scales, size_t scales_stride, size_t rows, size_t cols, void* d_out,
+                     int type, size_t stride, void* hip_stream);
+
+/* d_out (m x n, out_type, rows out_stride values apart) = the products of the rows of a (m x k) and of b (n x k), both held in blocks
+ * along k, + d_bias (n binary32 values, may be NULL), + what is in d_out (flag ZC_MX_ADD).  Sums in binary32, rounded once.
+ * The order of a sum depends on the sizes only, so that equal calls give equal results.
+ * d_ws: zc_mx_workspace_bytes(m, n, k) bytes, 16-byte aligned; its content is irrelevant, and calls that may overlap need one each. */
+#define ZC_MX_ADD 1u
+size_t zc_mx_workspace_bytes(size_t m, size_t n, size_t k);
+int zc_mx_product(const void* d_a, size_t a_stride, const void* d_a_scales, size_t a_scales_stride, const void* d_b, size_t b_stride,
+                  const void* d_b_scales, size_t b_scales_stride, size_t m, size_t n, size_t k, const float* d_bias, void* d_out, int out_type,
+                  size_t out_stride, unsigned flags, void* d_ws, size_t ws_bytes, void* hip_stream);
+
+/* The same with a = x (m x k values of x_type, rows x_stride values apart) quantised as by zc_mx_quantize: a layer on its activations,
+ * one token or many. */
+int zc_mx_linear(const void* d_x, int x_type, size_t x_stride, const void* d_w, size_t w_stride, const void* d_w_scales, size_t w_scales_stride,
+                 size_t m, size_t n, size_t k, const float* d_bias, void* d_out, int out_type, size_t out_stride, unsigned flags, void* d_ws,
+                 size_t ws_bytes, void* hip_stream);
+
 /* Completes an asynchronous call: synchronises hip_stream, returns the status of the last
  * call that used d_ws and stores its size result (total_bytes, or n for zc_decompress) in
  * *result (host, may be NULL).  d_ws NULL: the call was zc_compress_noalloc on the current device. */

@@ -27,6 +27,8 @@ EXPORTS = [
     "zc_reduce_compressed_ex", "zc_reduce_compressed_op", "zc_reduce_compressed_part", "zc_reduce_step_part", "zc_reduce_step", "zc_reduce_step_op", "zc_decompress_average", "zc_decompress_range",
     "zc_quality", "zc_finish", "zc_peek_header", "zc_strerror", "zc_debug_quantize", "zc_debug_block_offsets", "zc_debug_stream",
     "zc_profile_enable", "zc_profile_collect",
+    "zc_adamw", "zc_adamw_state_bytes", "zc_mx_codes_stride", "zc_mx_scales_stride", "zc_mx_quantize", "zc_mx_dequantize", "zc_mx_workspace_bytes",
+    "zc_mx_product", "zc_mx_linear",
 ]
 
 _lib = None
@@ -79,6 +81,17 @@ def lib():
         L.zc_debug_quantize.argtypes = [vp, sz, C.c_float, vp, vp, sz, vp]
         L.zc_debug_block_offsets.argtypes = [vp, sz, vp, sz, vp, sz, vp, u]
         L.zc_debug_stream.argtypes = [vp, vp, sz, C.c_int, C.c_int, vp]
+        i, d, u64 = C.c_int, C.c_double, C.c_uint64
+        for name in ("zc_adamw_state_bytes", "zc_mx_codes_stride", "zc_mx_scales_stride", "zc_mx_workspace_bytes"):
+            getattr(L, name).restype = sz
+        L.zc_adamw_state_bytes.argtypes = [vp, i, i]
+        L.zc_adamw.argtypes = [i, vp, vp, i, vp, i, vp, i, vp, sz, i, u64, d, d, d, d, d, vp, u64, vp]
+        L.zc_mx_codes_stride.argtypes = L.zc_mx_scales_stride.argtypes = [sz]
+        L.zc_mx_workspace_bytes.argtypes = [sz, sz, sz]
+        L.zc_mx_quantize.argtypes = [vp, i, sz, sz, sz, vp, sz, vp, sz, vp, sz, vp, sz, vp]
+        L.zc_mx_dequantize.argtypes = [vp, sz, vp, sz, sz, sz, vp, i, sz, vp]
+        L.zc_mx_product.argtypes = [vp, sz, vp, sz, vp, sz, vp, sz, sz, sz, sz, vp, vp, i, sz, u, vp, sz, vp]
+        L.zc_mx_linear.argtypes = [vp, i, sz, vp, sz, vp, sz, sz, sz, sz, vp, vp, i, sz, u, vp, sz, vp]
         L.zc_profile_enable.argtypes = [C.c_int]
         L.zc_profile_collect.argtypes = [C.POINTER(C.c_float), C.POINTER(C.c_int), C.c_int]
         _lib = L
@@ -377,3 +390,152 @@ def zc_profile_collect(cap=65536):
     if count < 0:
         raise ZcError(-count, "zc_profile_collect")
     return [(KERNEL_NAMES.get(kind[i], str(kind[i])), float(ms[i])) for i in range(count)]
+
+
+# ---- The calls around the collective.  Sizes, types and strides are the tensors' own; what does not fit together is ZC_ERR_ARG.
+
+ZC_F32, ZC_BF16, ZC_F16 = 0, 1, 2
+ZC_MX_ADD = 1
+_TYPES = {torch.float32: ZC_F32, torch.bfloat16: ZC_BF16, torch.float16: ZC_F16}
+
+
+def _words(values):
+    words = array("Q", values)
+    return words, words.buffer_info()[0] if words else None
+
+
+def zc_adamw_state_bytes(counts, state_bits=32):
+    """Bytes of the state of tensors with these numbers of values; 0 for what there is no state of."""
+    words, at = _words([int(n) for n in counts])
+    return int(lib().zc_adamw_state_bytes(at, len(words), int(state_bits)))
+
+
+def _one_type(tensors):
+    kinds = {t.dtype for t in tensors}
+    return _TYPES.get(kinds.pop(), -1) if len(kinds) == 1 else ZC_F32 if not kinds else -1
+
+
+def zc_adamw(d_params, d_grads, d_state, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, state_bits=32, seed=0, d_copies=None,
+             d_grad_scale=None, stream=None):
+    """One AdamW step over the tensors of the list d_params (contiguous, of one type; d_grads: as many of the same sizes, of one type), in place.
+    d_copies: None, or a list with a tensor or None for each.  Returns the status."""
+    k = len(d_params)
+    if len(d_grads) != k or (d_copies is not None and len(d_copies) != k):
+        return ZC_ERR_ARG
+    copies = [] if d_copies is None else [t for t in d_copies if t is not None]
+    sizes = [t.numel() for t in d_params]
+    if [t.numel() for t in d_grads] != sizes or not all(t.is_contiguous() for t in (*d_params, *d_grads, *copies)) or \
+            any(t is not None and t.numel() != n for t, n in zip(d_copies or (), sizes)) or \
+            (d_grad_scale is not None and (d_grad_scale.dtype != torch.float32 or d_grad_scale.numel() != 1)):
+        return ZC_ERR_ARG
+    lists = [_words(sizes), _words([t.data_ptr() for t in d_params]), _words([t.data_ptr() for t in d_grads]),
+             _words([t.data_ptr() if t is not None else 0 for t in d_copies]) if d_copies is not None else (None, None)]
+    if not 0 <= int(step) < 1 << 64 or not 0 <= int(seed) < 1 << 64:
+        return ZC_ERR_ARG
+    return lib().zc_adamw(k, lists[0][1], lists[1][1], _one_type(d_params), lists[2][1], _one_type(d_grads), lists[3][1], _one_type(copies),
+                          _p(d_state), _size(d_state) if d_state is not None else 0, int(state_bits), int(step), float(lr), float(beta1),
+                          float(beta2), float(eps), float(weight_decay), _p(d_grad_scale), int(seed), _stream(stream))
+
+
+def zc_mx_codes_stride(cols):
+    return int(lib().zc_mx_codes_stride(int(cols)))
+
+
+def zc_mx_scales_stride(cols):
+    return int(lib().zc_mx_scales_stride(int(cols)))
+
+
+def zc_mx_workspace_bytes(m, n, k):
+    return int(lib().zc_mx_workspace_bytes(int(m), int(n), int(k)))
+
+
+def _matrix(t):
+    """(address, type, rows, columns, values from row to row), or None for what is no matrix with its rows' values side by side."""
+    if t.dim() != 2 or t.dtype not in _TYPES:
+        return None
+    (rows, cols), (stride, one) = t.shape, t.stride()
+    if (cols > 1 and one != 1) or stride < 0:
+        return None
+    return t.data_ptr(), _TYPES[t.dtype], rows, cols, stride if rows > 1 else max(cols, stride)
+
+
+def _held(codes, scales, rows):
+    """(address, bytes from row to row) of the codes and of the scale bytes of a matrix of so many rows, or None."""
+    found = []
+    for t in (codes, scales):
+        if t.dim() != 2 or t.dtype != torch.uint8 or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1):
+            return None
+        if rows > 1 and t.stride(0) < t.shape[1]:
+            return None
+        found += [t.data_ptr(), t.stride(0) if rows > 1 else t.shape[1]]
+    return found
+
+
+def _covers(codes, scales, cols):
+    """Whether rows of codes and scale bytes have room for so many values."""
+    blocks = -(-cols // 32)
+    return codes.shape[1] >= 16 * blocks and scales.shape[1] >= blocks
+
+
+def zc_mx_quantize(d_in, d_codes, d_scales, d_codes_t=None, d_scales_t=None, stream=None):
+    """A matrix (its rows may lie apart) into 4-bit blocks along its rows (d_codes, d_scales: uint8 matrices with a row for each), along its columns
+    (d_codes_t, d_scales_t: a row for each column), or both.  Returns the status."""
+    x = _matrix(d_in)
+    if x is None:
+        return ZC_ERR_ARG
+    held = []
+    for codes, scales, rows, cols in ((d_codes, d_scales, x[2], x[3]), (d_codes_t, d_scales_t, x[3], x[2])):
+        if codes is None and scales is None:
+            held += [None, 0, None, 0]
+            continue
+        if codes is None or scales is None or not _covers(codes, scales, cols):
+            return ZC_ERR_ARG
+        one = _held(codes, scales, rows)
+        if one is None:
+            return ZC_ERR_ARG
+        held += one
+    return lib().zc_mx_quantize(*x, *held, _stream(stream))
+
+
+def zc_mx_dequantize(d_codes, d_scales, d_out, stream=None):
+    """What the blocks stand for, into the matrix d_out.  Returns the status."""
+    out = _matrix(d_out)
+    held = out and _held(d_codes, d_scales, out[2])
+    if not held or not _covers(d_codes, d_scales, out[3]):
+        return ZC_ERR_ARG
+    return lib().zc_mx_dequantize(*held, out[2], out[3], out[0], out[1], out[4], _stream(stream))
+
+
+def _product_end(d_w_codes, d_w_scales, k, d_out, d_bias):
+    """The operand b, the output and the bias of a product, checked against each other; None where they do not fit."""
+    out = _matrix(d_out)
+    if out is None or not _covers(d_w_codes, d_w_scales, k):
+        return None
+    held = _held(d_w_codes, d_w_scales, out[3])
+    if held is None or (d_bias is not None and (d_bias.dtype != torch.float32 or d_bias.numel() != out[3] or not d_bias.is_contiguous())):
+        return None
+    return out, held
+
+
+def zc_mx_product(d_a_codes, d_a_scales, d_b_codes, d_b_scales, k, d_out, d_ws, d_bias=None, add=False, stream=None):
+    """d_out (m x n) = a (m rows of k values, in blocks) times b (n rows) transposed, + d_bias, + d_out itself with add.  Returns the status."""
+    k = int(k)
+    end = _product_end(d_b_codes, d_b_scales, k, d_out, d_bias)
+    a = end and _held(d_a_codes, d_a_scales, end[0][2])
+    if not a or not _covers(d_a_codes, d_a_scales, k):
+        return ZC_ERR_ARG
+    out, b = end
+    return lib().zc_mx_product(*a, *b, out[2], out[3], k, _p(d_bias), out[0], out[1], out[4], ZC_MX_ADD if add else 0, _p(d_ws),
+                               _size(d_ws) if d_ws is not None else 0, _stream(stream))
+
+
+def zc_mx_linear(d_x, d_w_codes, d_w_scales, d_out, d_ws, d_bias=None, add=False, stream=None):
+    """d_out (m x n) = d_x (m x k values, quantised by the call) times the weights (n rows of k values, in blocks) transposed, + d_bias, + d_out itself
+    with add.  Returns the status."""
+    x = _matrix(d_x)
+    end = x and _product_end(d_w_codes, d_w_scales, x[3], d_out, d_bias)
+    if not end or end[0][2] != x[2]:
+        return ZC_ERR_ARG
+    out, w = end
+    return lib().zc_mx_linear(x[0], x[1], x[4], *w, out[2], out[3], x[3], _p(d_bias), out[0], out[1], out[4], ZC_MX_ADD if add else 0, _p(d_ws),
+                              _size(d_ws) if d_ws is not None else 0, _stream(stream))

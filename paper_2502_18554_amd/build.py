@@ -7,7 +7,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libzc.so")
-SOURCES = ["zc_api.hip"]
+SOURCES = ["zc_api.hip", "zc_layers.hip"]
 CALLS = os.path.join(HERE, "_zc_calls" + sysconfig.get_config_var("EXT_SUFFIX"))      # (named for this Python: another one leaves it alone)
 
 FLAGS = [

@@ -1,0 +1,223 @@
+// C ABI of the calls around the collective: the optimiser's step over many tensors, and layers held in 4-bit blocks.
+// Argument checks and launches.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "zc_adamw.h"
+#include "zc_mx.h"
+#include "zc_mx_product.h"
+
+using namespace zc;
+
+namespace {
+
+bool aligned(const void* p, u64 to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+bool type_valid(int type) { return type == ZC_F32 || type == ZC_BF16 || type == ZC_F16; }
+int launched() { return hipGetLastError() == hipSuccess ? ZC_OK : ZC_ERR_HIP; }
+constexpr u64 kMostGroups = 0x7fffffffu;
+
+template <int P, int G>
+void launch_adamw(const AdamwArgs& a, u32 tiles, int bits, hipStream_t stream) {
+  if (bits == 32) hipLaunchKernelGGL((adamw_kernel<P, G, 32>), dim3(tiles), dim3(kAdamwThreads), 0, stream, a);
+  else hipLaunchKernelGGL((adamw_kernel<P, G, 8>), dim3(tiles), dim3(kAdamwThreads), 0, stream, a);
+}
+template <int P>
+void launch_adamw(const AdamwArgs& a, u32 tiles, int bits, int grad_type, hipStream_t stream) {
+  if (grad_type == ZC_F32) launch_adamw<P, ZC_F32>(a, tiles, bits, stream);
+  else if (grad_type == ZC_BF16) launch_adamw<P, ZC_BF16>(a, tiles, bits, stream);
+  else launch_adamw<P, ZC_F16>(a, tiles, bits, stream);
+}
+void launch_adamw(const AdamwArgs& a, u32 tiles, int bits, int param_type, int grad_type, hipStream_t stream) {
+  if (param_type == ZC_F32) launch_adamw<ZC_F32>(a, tiles, bits, grad_type, stream);
+  else if (param_type == ZC_BF16) launch_adamw<ZC_BF16>(a, tiles, bits, grad_type, stream);
+  else launch_adamw<ZC_F16>(a, tiles, bits, grad_type, stream);
+}
+
+// Blocks of the tensors' state, or ~0 where sizes are out of range.
+u64 state_blocks(const size_t* n, int k) {
+  u64 blocks = 0;
+  for (int i = 0; i < k; ++i) {
+    if (n[i] > (u64(1) << 36)) return ~u64(0);
+    blocks += num_blocks(n[i]);
+  }
+  return blocks <= 0xffffffffu ? blocks : ~u64(0);
+}
+
+bool held_valid(const void* codes, const void* scales, u64 rows, u64 cols, u64 codes_stride, u64 scales_stride) {
+  const u64 blocks = num_blocks(cols);
+  if (codes_stride % 16 || scales_stride % 4 || codes_stride > (u64(1) << 32) || scales_stride > (u64(1) << 32)) return false;
+  if (codes_stride < kMxBytes * blocks || scales_stride < blocks) return false;
+  return rows == 0 || cols == 0 || (codes && scales && aligned(codes, 16) && aligned(scales, 4));
+}
+bool matrix_valid(const void* p, int type, u64 rows, u64 cols, u64 stride) {
+  return type_valid(type) && stride >= cols && stride <= (u64(1) << 32) && (rows == 0 || cols == 0 || (p && aligned(p, value_bytes(type))));
+}
+bool sizes_valid(u64 rows, u64 cols) { return rows <= 0x7fffffffu && cols <= 0x7fffffffu; }
+
+int product(const MxProductArgs& a, hipStream_t stream) {
+  if (a.m == 0 || a.n == 0) return ZC_OK;
+  const u64 down = (a.m + 15) / 16, across = (a.n + 15) / 16;
+  for (u64 at = 0; at < down; at += 65535) {                        // (a grid's second extent)
+    MxProductArgs part = a;
+    part.m = a.m - 16 * at;
+    part.a += 16 * at * a.a_stride;
+    part.a_scales += 16 * at * a.a_scales_stride;
+    part.out = static_cast<u8*>(a.out) + 16 * at * a.out_stride * value_bytes(a.out_type);
+    const u64 left = down - at;
+    hipLaunchKernelGGL(mx_product_kernel, dim3(u32(across), u32(left < 65535 ? left : 65535)), dim3(64), 0, stream, part);
+  }
+  return launched();
+}
+
+int quantize(const MxQuantizeArgs& a, hipStream_t stream) {
+  if (a.rows == 0 || a.cols == 0) return ZC_OK;
+  const u64 across = a.held.codes ? a.rows * num_blocks(a.cols) : 0, down = a.held_t.codes ? a.cols * num_blocks(a.rows) : 0;
+  const u64 groups = ((across > down ? across : down) + 255) / 256;
+  if (groups > kMostGroups) return ZC_ERR_ARG;
+  hipLaunchKernelGGL(mx_quantize_kernel, dim3(u32(groups)), dim3(256), 0, stream, a);
+  return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t zc_adamw_state_bytes(const size_t* n, int k, int state_bits) {
+  if (k < 0 || (k > 0 && !n) || (state_bits != 8 && state_bits != 32)) return 0;
+  const u64 blocks = state_blocks(n, k);
+  return blocks == ~u64(0) ? 0 : size_t(adamw_bytes(blocks, state_bits));
+}
+
+int zc_adamw(int k, const size_t* n, void* const* d_params, int param_type, const void* const* d_grads, int grad_type,
+             void* const* d_copies, int copy_type, void* d_state, size_t state_bytes, int state_bits, uint64_t step, double lr, double beta1,
+             double beta2, double eps, double weight_decay, const float* d_grad_scale, uint64_t seed, void* hip_stream) {
+  if (k < 0 || (k > 0 && (!n || !d_params || !d_grads)) || !type_valid(param_type) || !type_valid(grad_type)) return ZC_ERR_ARG;
+  if ((d_copies && !type_valid(copy_type)) || (state_bits != 8 && state_bits != 32) || step == 0) return ZC_ERR_ARG;
+  if (!(std::isfinite(lr) && lr >= 0 && beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1 && std::isfinite(eps) && eps >= 0 &&
+        std::isfinite(weight_decay) && weight_decay >= 0))
+    return ZC_ERR_ARG;
+  const u64 blocks = state_blocks(n, k);
+  if (blocks == ~u64(0) || state_bytes < adamw_bytes(blocks, state_bits) || (blocks && !d_state) || !aligned(d_state, 16)) return ZC_ERR_ARG;
+  if (!aligned(d_grad_scale, 4)) return ZC_ERR_ARG;
+  for (int i = 0; i < k; ++i) {
+    if (n[i] == 0) continue;
+    if (!d_params[i] || !d_grads[i] || !aligned(d_params[i], value_bytes(param_type)) || !aligned(d_grads[i], value_bytes(grad_type))) return ZC_ERR_ARG;
+    if (d_copies && !aligned(d_copies[i], value_bytes(copy_type))) return ZC_ERR_ARG;
+  }
+  AdamwArgs a = {};
+  a.c.b1 = float(beta1);
+  a.c.c1 = float(1 - beta1);
+  a.c.b2 = float(beta2);
+  a.c.c2 = float(1 - beta2);
+  a.c.keep = float(1 - lr * weight_decay);
+  a.c.rate = float(lr / (1 - std::pow(beta1, double(step))));
+  a.c.root = float(1 / std::sqrt(1 - std::pow(beta2, double(step))));
+  a.c.eps = float(eps);
+  a.copy_type = copy_type;
+  a.state = static_cast<u8*>(d_state);
+  a.blocks = blocks;
+  a.grad_scale = d_grad_scale;
+  a.key = adamw_key(seed, step);
+  a.stochastic = seed != 0;
+  u32 tiles = 0;
+  u64 block = 0;
+  const auto go = [&] {
+    launch_adamw(a, tiles, state_bits, param_type, grad_type, static_cast<hipStream_t>(hip_stream));
+    a.tensors = tiles = 0;
+  };
+  for (int i = 0; i < k; ++i) {
+    if (n[i] == 0) continue;
+    const u64 own = (n[i] + kAdamwTile - 1) / kAdamwTile;
+    if (a.tensors == kAdamwTensors || tiles + own > kMostGroups) go();
+    a.first_tile[a.tensors] = tiles;
+    a.tensor[a.tensors++] = {d_params[i], d_grads[i], d_copies ? d_copies[i] : nullptr, n[i], u32(block)};
+    tiles += u32(own);
+    block += num_blocks(n[i]);
+  }
+  if (a.tensors) go();
+  return launched();
+}
+
+size_t zc_mx_codes_stride(size_t cols) { return kMxBytes * num_blocks(cols); }
+size_t zc_mx_scales_stride(size_t cols) { return 4 * ((num_blocks(cols) + 3) / 4); }
+
+size_t zc_mx_workspace_bytes(size_t m, size_t n, size_t k) {
+  (void)n;
+  return pad16(m * zc_mx_codes_stride(k)) + pad16(m * zc_mx_scales_stride(k));
+}
+
+int zc_mx_quantize(const void* d_in, int type, size_t rows, size_t cols, size_t stride, void* d_codes, size_t codes_stride, void* d_scales,
+                   size_t scales_stride, void* d_codes_t, size_t codes_t_stride, void* d_scales_t, size_t scales_t_stride, void* hip_stream) {
+  if (!sizes_valid(rows, cols) || !matrix_valid(d_in, type, rows, cols, stride)) return ZC_ERR_ARG;
+  if ((!d_codes) != (!d_scales) || (!d_codes_t) != (!d_scales_t) || (!d_codes && !d_codes_t && rows && cols)) return ZC_ERR_ARG;
+  if (d_codes && !held_valid(d_codes, d_scales, rows, cols, codes_stride, scales_stride)) return ZC_ERR_ARG;
+  if (d_codes_t && !held_valid(d_codes_t, d_scales_t, cols, rows, codes_t_stride, scales_t_stride)) return ZC_ERR_ARG;
+  MxQuantizeArgs a;
+  a.in = d_in;
+  a.rows = rows, a.cols = cols, a.stride = stride;
+  a.type = type;
+  a.held = {static_cast<u8*>(d_codes), static_cast<u8*>(d_scales), codes_stride, scales_stride};
+  a.held_t = {static_cast<u8*>(d_codes_t), static_cast<u8*>(d_scales_t), codes_t_stride, scales_t_stride};
+  return quantize(a, static_cast<hipStream_t>(hip_stream));
+}
+
+int zc_mx_dequantize(const void* d_codes, size_t codes_stride, const void* d_scales, size_t scales_stride, size_t rows, size_t cols, void* d_out,
+                     int type, size_t stride, void* hip_stream) {
+  if (!sizes_valid(rows, cols) || !matrix_valid(d_out, type, rows, cols, stride)) return ZC_ERR_ARG;
+  if (!held_valid(d_codes, d_scales, rows, cols, codes_stride, scales_stride)) return ZC_ERR_ARG;
+  if (rows == 0 || cols == 0) return ZC_OK;
+  const u64 groups = (rows * num_blocks(cols) + 255) / 256;
+  if (groups > kMostGroups) return ZC_ERR_ARG;
+  MxDequantizeArgs a;
+  a.held = {static_cast<u8*>(const_cast<void*>(d_codes)), static_cast<u8*>(const_cast<void*>(d_scales)), codes_stride, scales_stride};
+  a.rows = rows, a.cols = cols, a.stride = stride;
+  a.out = d_out;
+  a.type = type;
+  hipLaunchKernelGGL(mx_dequantize_kernel, dim3(u32(groups)), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+  return launched();
+}
+
+int zc_mx_product(const void* d_a, size_t a_stride, const void* d_a_scales, size_t a_scales_stride, const void* d_b, size_t b_stride,
+                  const void* d_b_scales, size_t b_scales_stride, size_t m, size_t n, size_t k, const float* d_bias, void* d_out, int out_type,
+                  size_t out_stride, unsigned flags, void* d_ws, size_t ws_bytes, void* hip_stream) {
+  if (!sizes_valid(m, k) || !sizes_valid(n, k) || (flags & ~ZC_MX_ADD) || !matrix_valid(d_out, out_type, m, n, out_stride)) return ZC_ERR_ARG;
+  if (!held_valid(d_a, d_a_scales, m, k, a_stride, a_scales_stride) || !held_valid(d_b, d_b_scales, n, k, b_stride, b_scales_stride)) return ZC_ERR_ARG;
+  if (!aligned(d_bias, 4) || !aligned(d_ws, 16)) return ZC_ERR_ARG;
+  (void)ws_bytes;
+  MxProductArgs a;
+  a.a = static_cast<const u8*>(d_a), a.a_scales = static_cast<const u8*>(d_a_scales);
+  a.b = static_cast<const u8*>(d_b), a.b_scales = static_cast<const u8*>(d_b_scales);
+  a.a_stride = a_stride, a.a_scales_stride = a_scales_stride, a.b_stride = b_stride, a.b_scales_stride = b_scales_stride;
+  a.m = m, a.n = n;
+  a.blocks = u32(num_blocks(k));
+  a.bias = d_bias;
+  a.out = d_out;
+  a.out_stride = out_stride;
+  a.out_type = out_type;
+  a.add = flags & ZC_MX_ADD;
+  return product(a, static_cast<hipStream_t>(hip_stream));
+}
+
+int zc_mx_linear(const void* d_x, int x_type, size_t x_stride, const void* d_w, size_t w_stride, const void* d_w_scales, size_t w_scales_stride,
+                 size_t m, size_t n, size_t k, const float* d_bias, void* d_out, int out_type, size_t out_stride, unsigned flags, void* d_ws,
+                 size_t ws_bytes, void* hip_stream) {
+  if (!sizes_valid(m, k) || !matrix_valid(d_x, x_type, m, k, x_stride)) return ZC_ERR_ARG;
+  if (ws_bytes < zc_mx_workspace_bytes(m, n, k) || !aligned(d_ws, 16) || (!d_ws && m && k)) return ZC_ERR_ARG;
+  const u64 codes_stride = zc_mx_codes_stride(k), scales_stride = zc_mx_scales_stride(k), codes_bytes = pad16(m * codes_stride);
+  u8* const codes = static_cast<u8*>(d_ws);
+  u8* const scales = codes + codes_bytes;
+  // (the product's own checks come first: nothing is launched by a call that is refused)
+  if (!sizes_valid(n, k) || (flags & ~ZC_MX_ADD) || !matrix_valid(d_out, out_type, m, n, out_stride) || !aligned(d_bias, 4) ||
+      !held_valid(d_w, d_w_scales, n, k, w_stride, w_scales_stride))
+    return ZC_ERR_ARG;
+  if (n == 0) return ZC_OK;
+  if (k) {
+    const int st = zc_mx_quantize(d_x, x_type, m, k, x_stride, codes, codes_stride, scales, scales_stride, nullptr, 0, nullptr, 0, hip_stream);
+    if (st != ZC_OK) return st;
+  }
+  return zc_mx_product(codes, codes_stride, scales, scales_stride, d_w, w_stride, d_w_scales, w_scales_stride, m, n, k, d_bias, d_out, out_type,
+                       out_stride, flags, nullptr, 0, hip_stream);
+}
+
+}  // extern "C"
