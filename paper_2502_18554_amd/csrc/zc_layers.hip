@@ -55,8 +55,22 @@ bool matrix_valid(const void* p, int type, u64 rows, u64 cols, u64 stride) {
 }
 bool sizes_valid(u64 rows, u64 cols) { return rows <= 0x7fffffffu && cols <= 0x7fffffffu; }
 
+template <int T>
+void launch_tiles(const MxProductArgs& a, hipStream_t stream) {
+  const u64 down = (a.m + mx_tile_rows(T) - 1) / mx_tile_rows(T), across = (a.n + mx_tile_rows(T) - 1) / mx_tile_rows(T);
+  hipLaunchKernelGGL((mx_tile_kernel<T, T>), dim3(u32(down * across)), dim3(256), 0, stream, a, u32(down), u32(across));
+}
+
 int product(const MxProductArgs& a, hipStream_t stream) {
   if (a.m == 0 || a.n == 0) return ZC_OK;
+  if (a.blocks > 0 && a.m > 32 && a.a_stride <= kMostTileStride && a.b_stride <= kMostTileStride && a.a_scales_stride <= kMostTileStride && a.b_scales_stride <= kMostTileStride) {
+    const u64 t4 = ((a.m + 255) / 256) * ((a.n + 255) / 256), t2 = ((a.m + 127) / 128) * ((a.n + 127) / 128), t1 = ((a.m + 63) / 64) * ((a.n + 63) / 64);
+    if (t4 >= 200) launch_tiles<4>(a, stream);
+    else if (t2 >= 200) launch_tiles<2>(a, stream);
+    else launch_tiles<1>(a, stream);
+    (void)t1;
+    return launched();
+  }
   const u64 down = (a.m + 15) / 16, across = (a.n + 15) / 16;
   for (u64 at = 0; at < down; at += 65535) {                        // (a grid's second extent)
     MxProductArgs part = a;
