@@ -84,13 +84,18 @@ int product(const MxProductArgs& a, hipStream_t stream) {
   return launched();
 }
 
+template <int TYPE>
+int launch_quantize(const MxQuantizeArgs& a, hipStream_t stream) {
+  const u64 down = (a.rows + kMxTileRows - 1) / kMxTileRows, across = (a.cols + mx_tile_cols(TYPE) - 1) / mx_tile_cols(TYPE), tiles = down * across;
+  if (tiles > kMostGroups) return ZC_ERR_ARG;
+  if (a.held.codes && a.held_t.codes) hipLaunchKernelGGL((mx_quantize_kernel<TYPE, true, true>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(down), u32(tiles));
+  else if (a.held.codes) hipLaunchKernelGGL((mx_quantize_kernel<TYPE, true, false>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(down), u32(tiles));
+  else hipLaunchKernelGGL((mx_quantize_kernel<TYPE, false, true>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(down), u32(tiles));
+  return launched();
+}
 int quantize(const MxQuantizeArgs& a, hipStream_t stream) {
   if (a.rows == 0 || a.cols == 0) return ZC_OK;
-  const u64 across = a.held.codes ? a.rows * num_blocks(a.cols) : 0, down = a.held_t.codes ? a.cols * num_blocks(a.rows) : 0;
-  const u64 groups = ((across > down ? across : down) + 255) / 256;
-  if (groups > kMostGroups) return ZC_ERR_ARG;
-  hipLaunchKernelGGL(mx_quantize_kernel, dim3(u32(groups)), dim3(256), 0, stream, a);
-  return launched();
+  return a.type == ZC_F32 ? launch_quantize<ZC_F32>(a, stream) : a.type == ZC_BF16 ? launch_quantize<ZC_BF16>(a, stream) : launch_quantize<ZC_F16>(a, stream);
 }
 
 }  // namespace
@@ -181,14 +186,19 @@ int zc_mx_dequantize(const void* d_codes, size_t codes_stride, const void* d_sca
   if (!sizes_valid(rows, cols) || !matrix_valid(d_out, type, rows, cols, stride)) return ZC_ERR_ARG;
   if (!held_valid(d_codes, d_scales, rows, cols, codes_stride, scales_stride)) return ZC_ERR_ARG;
   if (rows == 0 || cols == 0) return ZC_OK;
-  const u64 groups = (rows * num_blocks(cols) + 255) / 256;
-  if (groups > kMostGroups) return ZC_ERR_ARG;
-  MxDequantizeArgs a;
-  a.held = {static_cast<u8*>(const_cast<void*>(d_codes)), static_cast<u8*>(const_cast<void*>(d_scales)), codes_stride, scales_stride};
-  a.rows = rows, a.cols = cols, a.stride = stride;
-  a.out = d_out;
-  a.type = type;
-  hipLaunchKernelGGL(mx_dequantize_kernel, dim3(u32(groups)), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+  const u32 across = u32((cols + 7) / 8);
+  const u64 most = 0xf0000000u / across;                            // rows whose pieces, and those of the last workgroup and row behind them, are counted in 32 bits
+  for (u64 at = 0; at < rows; at += most) {
+    const u64 now = rows - at < most ? rows - at : most;
+    MxDequantizeArgs a;
+    a.held = {static_cast<u8*>(const_cast<void*>(d_codes)) + at * codes_stride, static_cast<u8*>(const_cast<void*>(d_scales)) + at * scales_stride, codes_stride, scales_stride};
+    a.rows = now, a.cols = cols, a.stride = stride;
+    a.out = static_cast<u8*>(d_out) + at * stride * value_bytes(type);
+    a.type = type;
+    const u32 pieces = u32(now * across);
+    const u32 groups = u32((u64(pieces) + 256 * kMxPieces - 1) / (256 * kMxPieces));
+    hipLaunchKernelGGL(mx_dequantize_kernel, dim3(groups), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a, across, u32(((u64(1) << 32) + across - 1) / across), pieces);
+  }
   return launched();
 }
 

@@ -15,13 +15,61 @@ __device__ inline u32 mx_scale(u32 top) {
   return e == 255u ? 255u : e > 2u ? e - 2u : 0u;
 }
 
-// Eight values (scaled by the block's power of two in the conversion) as eight codes, the first one lowest.
-__device__ inline u32 mx_codes(const float (&v)[8], float scale) {
-  u32 w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], scale, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], scale, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], scale, 2);
-  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
+// Values of a type by the 16 bytes, as they lie in memory.
+template <int TYPE> struct MxPack;
+template <> struct MxPack<ZC_F32> {
+  static constexpr u32 kValues = 4;
+  static __device__ u32 top(u32x4_t w) {
+    const u32x4_t m = w & 0x7fffffffu;
+    return max(max(m[0], m[1]), max(m[2], m[3]));
+  }
+  static __device__ u32 top_value(u32 top) { return top; }                  // the largest magnitude in binary32, from what top() gave
+};
+// Magnitudes of two 16-bit values compared side by side.
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+__device__ inline u32 max_pairs(u32 a, u32 b) {
+  return __builtin_bit_cast(u32, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, a), __builtin_bit_cast(u16x2_t, b)));
+}
+template <> struct MxPack<ZC_BF16> {
+  static constexpr u32 kValues = 8;
+  static __device__ u32 top(u32x4_t w) {
+    const u32x4_t m = w & 0x7fff7fffu;
+    return max_pairs(max_pairs(m[0], m[1]), max_pairs(m[2], m[3]));
+  }
+  static __device__ u32 top_value(u32 top) { return max(top << 16, top & 0xffff0000u); }
+};
+template <> struct MxPack<ZC_F16> {
+  static constexpr u32 kValues = 8;
+  static __device__ u32 top(u32x4_t w) { return MxPack<ZC_BF16>::top(w); }
+  static __device__ u32 top_value(u32 top) {
+    const u16 high = u16(max(top & 0xffffu, top >> 16));
+    return __float_as_uint(float(__builtin_bit_cast(_Float16, high)));
+  }
+};
+
+// Eight values, in the order of their words, as eight codes, the first one lowest; the conversion divides by the block's power of two.
+template <int TYPE>
+__device__ inline u32 mx_codes(const u32 (&w)[TYPE == ZC_F32 ? 8 : 4], float scale) {
+  u32 c = 0;
+  if constexpr (TYPE == ZC_F32) {
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(w[0]), __uint_as_float(w[1]), scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(w[2]), __uint_as_float(w[3]), scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(w[4]), __uint_as_float(w[5]), scale, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(w[6]), __uint_as_float(w[7]), scale, 3);
+  } else if constexpr (TYPE == ZC_BF16) {
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(pair, w[0]), scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(pair, w[1]), scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(pair, w[2]), scale, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(pair, w[3]), scale, 3);
+  } else {
+    typedef _Float16 pair __attribute__((ext_vector_type(2)));
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(pair, w[0]), scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(pair, w[1]), scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(pair, w[2]), scale, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(pair, w[3]), scale, 3);
+  }
+  return c;
 }
 
 __device__ inline void mx_values(u32 codes, float scale, float (&v)[8]) {
@@ -45,37 +93,107 @@ struct MxQuantizeArgs {
   MxHeld held, held_t;          // null codes: not wanted
 };
 
-// One thread a block: along a row, or down a column for the transposed matrix.
-__device__ inline void mx_quantize_block(const MxQuantizeArgs& a, u64 row, u64 col, u64 row_step, u64 col_step, u64 count, u8* codes, u8* scale) {
-  float v[32];
+// A workgroup takes 128 rows of 256 bytes (128 values of 16 bits, 64 of 32).  Eight threads a row hold 32 bytes each and make the blocks along the row
+// from their registers, two or four of them a block.  For the blocks down the columns the tile goes through LDS: wave w takes rows 32 w .. 32 w + 31, a
+// lane one column (of 32 bits) or two (of 16).  Memory sees every value once, whichever of the two are wanted.
+// Tiles follow each other down the matrix, so that what one XCD writes of a row of the transposed matrix lies together.
+constexpr u32 kMxTileRows = 128, kMxTileBytes = 256;
+__host__ __device__ constexpr u32 mx_tile_cols(int type) { return kMxTileBytes / (type == ZC_F32 ? 4 : 2); }
+
+struct __attribute__((packed, aligned(2))) MxSixteen { u32 w[4]; };
+
+template <int TYPE, bool ALONG, bool DOWN>
+__global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 tiles_down, u32 tiles) {
+  using One = typename ValueOf<TYPE>::One;
+  using Pack = MxPack<TYPE>;
+  constexpr u32 N = 2 * Pack::kValues, COLS = mx_tile_cols(TYPE), LANES = kBlockValues / N;       // values of a thread, of a row; threads of a block
+  __shared__ u32x4_t tile[DOWN ? kMxTileRows * kMxTileBytes / 16 : 1];
+  const u32 tid = threadIdx.x, part = tid & 7u;
+  const u32 xcd = blockIdx.x & 7u, t = xcd * (tiles >> 3) + min(xcd, tiles & 7u) + (blockIdx.x >> 3);
+  const u32 across = t / tiles_down;
+  const u64 row0 = u64(t - across * tiles_down) * kMxTileRows, col0 = u64(across) * COLS;
+  const u64 col = col0 + part * N;
+#pragma unroll
+  for (u32 i = 0; i < 4; ++i) {
+    const u32 in_tile = 32 * i + (tid >> 3);
+    const u64 row = row0 + in_tile;
+    u32x4_t w[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    if (row < a.rows) {
+      const One* const p = static_cast<const One*>(a.in) + row * a.stride + col;
+      if (col + N <= a.cols) {
+#pragma unroll
+        for (u32 h = 0; h < 2; ++h) {
+          const MxSixteen s = reinterpret_cast<const MxSixteen*>(p)[h];
+          w[h] = u32x4_t{s.w[0], s.w[1], s.w[2], s.w[3]};
+        }
+      } else if (col < a.cols) {
+#pragma unroll
+        for (u32 j = 0; j < N; ++j) {
+          if (col + j >= a.cols) continue;
+          if constexpr (TYPE == ZC_F32) w[j / 4][j % 4] = __float_as_uint(p[j]);
+          else w[j / 8][j / 2 % 4] |= u32(__builtin_bit_cast(u16, p[j])) << (16 * (j & 1u));
+        }
+      }
+    }
+    if (DOWN) {
+      tile[in_tile * 16 + part * 2] = w[0];
+      tile[in_tile * 16 + part * 2 + 1] = w[1];
+    }
+    if (ALONG) {
+      u32 top = Pack::top_value(TYPE == ZC_F32 ? max(Pack::top(w[0]), Pack::top(w[1])) : max_pairs(Pack::top(w[0]), Pack::top(w[1])));
+      top = max(top, u32(__builtin_amdgcn_update_dpp(0, int(top), 0xB1, 0xf, 0xf, true)));                    // quad_perm 1 0 3 2
+      if (LANES == 4) top = max(top, u32(__builtin_amdgcn_update_dpp(0, int(top), 0x4E, 0xf, 0xf, true)));    // quad_perm 2 3 0 1
+      const u32 s = mx_scale(top);
+      const float scale = scale_value(s);
+      const u64 block = col / kBlockValues;
+      if (row < a.rows && block * kBlockValues < a.cols) {
+        u8* const codes = a.held.codes + row * a.held.codes_stride + col / 2;
+        if constexpr (TYPE == ZC_F32) {
+          const u32 eight[8] = {w[0][0], w[0][1], w[0][2], w[0][3], w[1][0], w[1][1], w[1][2], w[1][3]};
+          *reinterpret_cast<u32*>(codes) = s == 255u ? 0u : mx_codes<TYPE>(eight, scale);
+        } else {
+          const u32 low[4] = {w[0][0], w[0][1], w[0][2], w[0][3]}, high[4] = {w[1][0], w[1][1], w[1][2], w[1][3]};
+          *reinterpret_cast<u32x2_t*>(codes) = s == 255u ? u32x2_t{0, 0} : u32x2_t{mx_codes<TYPE>(low, scale), mx_codes<TYPE>(high, scale)};
+        }
+        if (part % LANES == 0) a.held.scales[row * a.held.scales_stride + block] = u8(s);
+      }
+    }
+  }
+  if (!DOWN) return;
+  __syncthreads();
+  const u32 lane = tid & 63u, wave = tid >> 6;
+  const u64 block = row0 / kBlockValues + wave;
+  if (block * kBlockValues >= a.rows) return;
+  const u32* const words = reinterpret_cast<const u32*>(tile) + wave * (32 * kMxTileBytes / 4) + lane;
+  u32 v[32];
   u32 top = 0;
 #pragma unroll
-  for (u32 j = 0; j < 32; ++j) {
-    v[j] = j < count ? load_value(a.in, a.type, (row + j * row_step) * a.stride + col + j * col_step) : 0.0f;
-    top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+  for (u32 r = 0; r < 32; ++r) {
+    v[r] = words[r * (kMxTileBytes / 4)];
+    top = TYPE == ZC_F32 ? max(top, v[r] & 0x7fffffffu) : max_pairs(top, v[r] & 0x7fff7fffu);
   }
-  const u32 s = mx_scale(top);
-  *scale = u8(s);
-  u32x4_t w;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float part[8] = {v[8 * i], v[8 * i + 1], v[8 * i + 2], v[8 * i + 3], v[8 * i + 4], v[8 * i + 5], v[8 * i + 6], v[8 * i + 7]};
-    w[i] = s == 255u ? 0u : mx_codes(part, scale_value(s));
-  }
-  *reinterpret_cast<u32x4_t*>(codes) = w;
-}
-
-__global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a) {
-  const u64 i = u64(blockIdx.x) * 256 + threadIdx.x;
-  const u64 across = num_blocks(a.cols), down = num_blocks(a.rows);
-  if (a.held.codes && i < a.rows * across) {
-    const u64 r = i / across, b = i % across;
-    mx_quantize_block(a, r, 32 * b, 0, 1, a.cols - 32 * b, a.held.codes + r * a.held.codes_stride + kMxBytes * b, a.held.scales + r * a.held.scales_stride + b);
-  }
-  if (a.held_t.codes && i < a.cols * down) {
-    const u64 b = i / a.cols, col = i % a.cols;
-    mx_quantize_block(a, 32 * b, col, 1, 0, a.rows - 32 * b, a.held_t.codes + col * a.held_t.codes_stride + kMxBytes * b,
-                      a.held_t.scales + col * a.held_t.scales_stride + b);
+  for (u32 h = 0; h < (TYPE == ZC_F32 ? 1u : 2u); ++h) {
+    const u64 c = col0 + (TYPE == ZC_F32 ? lane : 2 * lane + h);
+    if (c >= a.cols) break;
+    const u32 s = mx_scale(TYPE == ZC_F32 ? top : Pack::top_value(h ? top >> 16 : top & 0xffffu));
+    const float scale = scale_value(s);
+    u32x4_t codes;
+#pragma unroll
+    for (u32 q = 0; q < 4; ++q) {
+      if constexpr (TYPE == ZC_F32) {
+        const u32 eight[8] = {v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3], v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]};
+        codes[q] = mx_codes<TYPE>(eight, scale);
+      } else {
+        u32 four[4];                                    // two rows' values of the column side by side
+#pragma unroll
+        for (u32 j = 0; j < 4; ++j) four[j] = __builtin_amdgcn_perm(v[8 * q + 2 * j + 1], v[8 * q + 2 * j], h ? 0x07060302u : 0x05040100u);
+        codes[q] = mx_codes<TYPE>(four, scale);
+      }
+    }
+    if (s == 255u) codes = u32x4_t{0, 0, 0, 0};
+    *reinterpret_cast<u32x4_t*>(a.held_t.codes + c * a.held_t.codes_stride + kMxBytes * block) = codes;
+    a.held_t.scales[c * a.held_t.scales_stride + block] = u8(s);
   }
 }
 
@@ -86,21 +204,32 @@ struct MxDequantizeArgs {
   int type;
 };
 
-__global__ __launch_bounds__(256) void mx_dequantize_kernel(MxDequantizeArgs a) {
-  const u64 i = u64(blockIdx.x) * 256 + threadIdx.x;
-  const u64 across = num_blocks(a.cols);
-  if (i >= a.rows * across) return;
-  const u64 r = i / across, b = i % across;
-  const u32x4_t w = *reinterpret_cast<const u32x4_t*>(a.held.codes + r * a.held.codes_stride + kMxBytes * b);
-  const float scale = scale_value(a.held.scales[r * a.held.scales_stride + b]);
-  const u64 count = a.cols - 32 * b;
+// Four bytes of codes a thread and step: eight values, so that a wave's stores follow each other.  Pieces of eight are counted through the rows, `across` of them a
+// row; a quotient by it is a product with `inverse` (2^32 / across rounded up), one too large at most.
+constexpr u32 kMxPieces = 4;
+
+__global__ __launch_bounds__(256) void mx_dequantize_kernel(MxDequantizeArgs a, u32 across, u32 inverse, u32 pieces) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+  for (u32 u = 0; u < kMxPieces; ++u) {
+    const u32 i = (blockIdx.x * kMxPieces + u) * 256u + threadIdx.x;
+    if (i >= pieces) return;
+    u32 row = across == 1 ? i : __umulhi(i, inverse);
+    if (row * across > i) --row;
+    const u32 piece = i - row * across;
+    const u32 w = *reinterpret_cast<const u32*>(a.held.codes + row * a.held.codes_stride + 4 * u64(piece));
+    const float scale = scale_value(a.held.scales[row * a.held.scales_stride + piece / 4]);
     float v[8];
-    mx_values(w[q], scale, v);
+    mx_values(w, scale, v);
+    const u64 col = 8 * u64(piece), at = row * a.stride + col;
+    if (col + 8 <= a.cols) {
+      const float low[4] = {v[0], v[1], v[2], v[3]}, high[4] = {v[4], v[5], v[6], v[7]};
+      store_four(a.out, a.type, at, low);
+      store_four(a.out, a.type, at + 4, high);
+    } else {
 #pragma unroll
-    for (u32 j = 0; j < 8; ++j)
-      if (8 * q + j < count) store_value(a.out, a.type, r * a.stride + 32 * b + 8 * q + j, v[j]);
+      for (u32 j = 0; j < 8; ++j)
+        if (col + j < a.cols) store_value(a.out, a.type, at + j, v[j]);
+    }
   }
 }
 
