@@ -33,6 +33,7 @@ EXPORTS = [
 
 _lib = None
 _native = None       # csrc/zc_calls.cpp: the same calls for arguments of the plainest form (NotImplemented for others), once libzc.so is loaded
+_native_layers = None    # csrc/zc_layer_calls.cpp, likewise for the layer calls
 
 
 class ZcError(RuntimeError):
@@ -100,7 +101,7 @@ def lib():
 
 
 def _load_native(L):
-    global _native
+    global _native, _native_layers
     path = os.path.join(_HERE, "_zc_calls" + sysconfig.get_config_var("EXT_SUFFIX"))      # (the one that was built for this Python)
     stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     if not os.path.exists(path) or stream_of is None:
@@ -114,6 +115,11 @@ def _load_native(L):
     calls = (L.zc_compress_ex, L.zc_decompress_ex, L.zc_reduce_compressed_op, L.zc_reduce_step_op, L.zc_decompress_many)
     native.setup(*(C.cast(f, C.c_void_p).value for f in calls), torch._C._cuda_getDevice, stream_of)
     _native = native
+    setup = getattr(native, "setup_layers", None)
+    if setup:
+        calls = (L.zc_adamw, L.zc_mx_quantize, L.zc_mx_dequantize, L.zc_mx_product, L.zc_mx_linear)
+        if setup(*(C.cast(f, C.c_void_p).value for f in calls), str(torch.__version__).split("+")[0]):
+            _native_layers = native
 
 
 # Small calls are bound by what happens here (a chunk of a few thousand values runs for 4 us).  Where ctypes takes a call, addresses go to
@@ -392,7 +398,7 @@ def zc_profile_collect(cap=65536):
     return [(KERNEL_NAMES.get(kind[i], str(kind[i])), float(ms[i])) for i in range(count)]
 
 
-# ---- The calls around the collective.  Sizes, types and strides are the tensors' own; what does not fit together is ZC_ERR_ARG.
+# ---- The calls around the collective.  Sizes, types and strides are the tensors' own; what does not fit together, or is not on the GPU, is ZC_ERR_ARG.
 
 ZC_F32, ZC_BF16, ZC_F16 = 0, 1, 2
 ZC_MX_ADD = 1
@@ -419,14 +425,19 @@ def zc_adamw(d_params, d_grads, d_state, step, lr, beta1=0.9, beta2=0.999, eps=1
              d_grad_scale=None, stream=None):
     """One AdamW step over the tensors of the list d_params (contiguous, of one type; d_grads: as many of the same sizes, of one type), in place.
     d_copies: None, or a list with a tensor or None for each.  Returns the status."""
+    lib()
+    if _native_layers:
+        r = _native_layers.adamw(d_params, d_grads, d_state, step, lr, beta1, beta2, eps, weight_decay, state_bits, seed, d_copies, d_grad_scale, stream)
+        if r is not NotImplemented:
+            return r
     k = len(d_params)
     if len(d_grads) != k or (d_copies is not None and len(d_copies) != k):
         return ZC_ERR_ARG
     copies = [] if d_copies is None else [t for t in d_copies if t is not None]
     sizes = [t.numel() for t in d_params]
-    if [t.numel() for t in d_grads] != sizes or not all(t.is_contiguous() for t in (*d_params, *d_grads, *copies)) or \
+    if [t.numel() for t in d_grads] != sizes or not all(t.is_contiguous() and t.is_cuda for t in (*d_params, *d_grads, *copies)) or \
             any(t is not None and t.numel() != n for t, n in zip(d_copies or (), sizes)) or \
-            (d_grad_scale is not None and (d_grad_scale.dtype != torch.float32 or d_grad_scale.numel() != 1)):
+            not all(t is None or t.is_cuda for t in (d_state, d_grad_scale)) or (d_grad_scale is not None and (d_grad_scale.dtype != torch.float32 or d_grad_scale.numel() != 1)):
         return ZC_ERR_ARG
     lists = [_words(sizes), _words([t.data_ptr() for t in d_params]), _words([t.data_ptr() for t in d_grads]),
              _words([t.data_ptr() if t is not None else 0 for t in d_copies]) if d_copies is not None else (None, None)]
@@ -451,7 +462,7 @@ def zc_mx_workspace_bytes(m, n, k):
 
 def _matrix(t):
     """(address, type, rows, columns, values from row to row), or None for what is no matrix with its rows' values side by side."""
-    if t.dim() != 2 or t.dtype not in _TYPES:
+    if t.dim() != 2 or t.dtype not in _TYPES or not t.is_cuda:
         return None
     (rows, cols), (stride, one) = t.shape, t.stride()
     if (cols > 1 and one != 1) or stride < 0:
@@ -463,7 +474,7 @@ def _held(codes, scales, rows):
     """(address, bytes from row to row) of the codes and of the scale bytes of a matrix of so many rows, or None."""
     found = []
     for t in (codes, scales):
-        if t.dim() != 2 or t.dtype != torch.uint8 or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1):
+        if t.dim() != 2 or t.dtype != torch.uint8 or not t.is_cuda or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1):
             return None
         if rows > 1 and t.stride(0) < t.shape[1]:
             return None
@@ -480,6 +491,11 @@ def _covers(codes, scales, cols):
 def zc_mx_quantize(d_in, d_codes, d_scales, d_codes_t=None, d_scales_t=None, stream=None):
     """A matrix (its rows may lie apart) into 4-bit blocks along its rows (d_codes, d_scales: uint8 matrices with a row for each), along its columns
     (d_codes_t, d_scales_t: a row for each column), or both.  Returns the status."""
+    lib()
+    if _native_layers:
+        r = _native_layers.quantize(d_in, d_codes, d_scales, d_codes_t, d_scales_t, stream)
+        if r is not NotImplemented:
+            return r
     x = _matrix(d_in)
     if x is None:
         return ZC_ERR_ARG
@@ -499,6 +515,11 @@ def zc_mx_quantize(d_in, d_codes, d_scales, d_codes_t=None, d_scales_t=None, str
 
 def zc_mx_dequantize(d_codes, d_scales, d_out, stream=None):
     """What the blocks stand for, into the matrix d_out.  Returns the status."""
+    lib()
+    if _native_layers:
+        r = _native_layers.dequantize(d_codes, d_scales, d_out, stream)
+        if r is not NotImplemented:
+            return r
     out = _matrix(d_out)
     held = out and _held(d_codes, d_scales, out[2])
     if not held or not _covers(d_codes, d_scales, out[3]):
@@ -512,17 +533,22 @@ def _product_end(d_w_codes, d_w_scales, k, d_out, d_bias):
     if out is None or not _covers(d_w_codes, d_w_scales, k):
         return None
     held = _held(d_w_codes, d_w_scales, out[3])
-    if held is None or (d_bias is not None and (d_bias.dtype != torch.float32 or d_bias.numel() != out[3] or not d_bias.is_contiguous())):
+    if held is None or (d_bias is not None and (d_bias.dtype != torch.float32 or not d_bias.is_cuda or d_bias.numel() != out[3] or not d_bias.is_contiguous())):
         return None
     return out, held
 
 
 def zc_mx_product(d_a_codes, d_a_scales, d_b_codes, d_b_scales, k, d_out, d_ws, d_bias=None, add=False, stream=None):
     """d_out (m x n) = a (m rows of k values, in blocks) times b (n rows) transposed, + d_bias, + d_out itself with add.  Returns the status."""
+    lib()
+    if _native_layers:
+        r = _native_layers.product(d_a_codes, d_a_scales, d_b_codes, d_b_scales, k, d_out, d_ws, d_bias, add, stream)
+        if r is not NotImplemented:
+            return r
     k = int(k)
     end = _product_end(d_b_codes, d_b_scales, k, d_out, d_bias)
     a = end and _held(d_a_codes, d_a_scales, end[0][2])
-    if not a or not _covers(d_a_codes, d_a_scales, k):
+    if not a or not _covers(d_a_codes, d_a_scales, k) or not (d_ws is None or d_ws.is_cuda):
         return ZC_ERR_ARG
     out, b = end
     return lib().zc_mx_product(*a, *b, out[2], out[3], k, _p(d_bias), out[0], out[1], out[4], ZC_MX_ADD if add else 0, _p(d_ws),
@@ -532,9 +558,14 @@ def zc_mx_product(d_a_codes, d_a_scales, d_b_codes, d_b_scales, k, d_out, d_ws, 
 def zc_mx_linear(d_x, d_w_codes, d_w_scales, d_out, d_ws, d_bias=None, add=False, stream=None):
     """d_out (m x n) = d_x (m x k values, quantised by the call) times the weights (n rows of k values, in blocks) transposed, + d_bias, + d_out itself
     with add.  Returns the status."""
+    lib()
+    if _native_layers:
+        r = _native_layers.linear(d_x, d_w_codes, d_w_scales, d_out, d_ws, d_bias, add, stream)
+        if r is not NotImplemented:
+            return r
     x = _matrix(d_x)
     end = x and _product_end(d_w_codes, d_w_scales, x[3], d_out, d_bias)
-    if not end or end[0][2] != x[2]:
+    if not end or end[0][2] != x[2] or not (d_ws is None or d_ws.is_cuda):
         return ZC_ERR_ARG
     out, w = end
     return lib().zc_mx_linear(x[0], x[1], x[4], *w, out[2], out[3], x[3], _p(d_bias), out[0], out[1], out[4], ZC_MX_ADD if add else 0, _p(d_ws),

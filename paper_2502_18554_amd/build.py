@@ -1,4 +1,5 @@
 """Build the HIP library (csrc/*.hip -> libzc.so) for gfx950 with hipcc, and the native calls of the binding for this Python, in-tree."""
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -36,10 +37,22 @@ def build_calls(verbose=False):
     if not os.path.exists(os.path.join(include, "Python.h")) or not shutil.which("g++"):
         print("no headers of this Python or no g++: the binding goes through ctypes alone")
         return
-    cmd = ["g++", "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", "-I" + include, os.path.join(CSRC, "zc_calls.cpp"), "-o", CALLS]
+    cmd = ["g++", "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", "-I" + include, os.path.join(CSRC, "zc_calls.cpp"), *layer_calls(), "-o", CALLS]
     if verbose:
         print(" ".join(cmd))
     subprocess.run(cmd, check=True)
+
+
+def layer_calls():
+    """What the native calls that read torch's tensors add to the command: nothing where torch's headers are not there (those calls go through ctypes then)."""
+    spec = importlib.util.find_spec("torch")
+    home = os.path.dirname(spec.origin) if spec and spec.origin else ""
+    headers, libraries = os.path.join(home, "include"), os.path.join(home, "lib")
+    if not os.path.exists(os.path.join(headers, "torch", "csrc", "autograd", "python_variable.h")) or not os.path.exists(os.path.join(libraries, "libtorch_python.so")):
+        print("no headers of torch: the layer calls go through ctypes")
+        return []
+    return ["-isystem", headers, "-isystem", os.path.join(headers, "torch", "csrc", "api", "include"), os.path.join(CSRC, "zc_layer_calls.cpp"),
+            "-L" + libraries, "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
 if __name__ == "__main__":

@@ -94,6 +94,10 @@ bool own_capacity(PyObject* given, PyObject* tensor, bool elements, uint64_t& v)
   return tensor == Py_None || of_method(tensor, g_numel, v);
 }
 
+}  // namespace
+
+namespace zc_calls {
+PyMethodDef* layer_methods() __attribute__((weak));      // zc_layer_calls.cpp, where it is built along
 // The stream as given, or the current one.
 bool stream_of(PyObject* given, void*& stream) {
   uint64_t v = 0;
@@ -112,6 +116,10 @@ bool stream_of(PyObject* given, void*& stream) {
   stream = reinterpret_cast<void*>(v);
   return ok;
 }
+}  // namespace zc_calls
+
+namespace {
+using zc_calls::stream_of;
 
 PyObject* not_this_way() {
   if (PyErr_Occurred()) return nullptr;
@@ -328,5 +336,10 @@ PyMODINIT_FUNC PyInit__zc_calls() {
   g_numel = PyUnicode_InternFromString("numel");
   g_cuda_stream = PyUnicode_InternFromString("cuda_stream");
   if (!g_data_ptr || !g_nbytes || !g_numel || !g_cuda_stream) return nullptr;
-  return PyModule_Create(&g_module);
+  PyObject* const module = PyModule_Create(&g_module);
+  if (module && zc_calls::layer_methods && PyModule_AddFunctions(module, zc_calls::layer_methods()) < 0) {
+    Py_DECREF(module);
+    return nullptr;
+  }
+  return module;
 }

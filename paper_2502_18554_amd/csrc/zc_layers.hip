@@ -6,6 +6,7 @@
 
 #include "zc_adamw.h"
 #include "zc_mx.h"
+#include "zc_mx_few.h"
 #include "zc_mx_product.h"
 
 using namespace zc;
@@ -61,9 +62,30 @@ void launch_tiles(const MxProductArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL((mx_tile_kernel<T, T>), dim3(u32(down * across)), dim3(256), 0, stream, a, u32(down), u32(across));
 }
 
+// Few rows: as many columns a workgroup as leave a workgroup for every CU.
+template <int RG, int CG, int X>
+void launch_few(const MxFewArgs& a, hipStream_t stream) {
+  const u64 groups = (a.p.n + 16 * CG - 1) / (16 * CG), spans = (a.p.blocks + kSpanOfBlocks - 1) / kSpanOfBlocks;
+  const u32 waves = spans < 1 ? 1u : spans < kFewWaves ? u32(spans) : kFewWaves;
+  hipLaunchKernelGGL((mx_few_kernel<RG, CG, X>), dim3(u32(groups)), dim3(64 * waves), 0, stream, a);
+}
+template <int RG, int X>
+void launch_few(const MxFewArgs& a, hipStream_t stream) {
+  if (a.p.n >= 4 * 16 * 256) launch_few<RG, 4, X>(a, stream);
+  else if (a.p.n >= 2 * 16 * 256) launch_few<RG, 2, X>(a, stream);
+  else launch_few<RG, 1, X>(a, stream);
+}
+template <int X>
+int launch_few(const MxFewArgs& a, hipStream_t stream) {
+  if (a.p.m <= 16) launch_few<1, X>(a, stream);
+  else launch_few<2, X>(a, stream);
+  return launched();
+}
+
 int product(const MxProductArgs& a, hipStream_t stream) {
   if (a.m == 0 || a.n == 0) return ZC_OK;
-  if (a.blocks > 0 && a.m > 32 && a.a_stride <= kMostTileStride && a.b_stride <= kMostTileStride && a.a_scales_stride <= kMostTileStride && a.b_scales_stride <= kMostTileStride) {
+  if (a.m <= kFewRows) return launch_few<kHeldRows>(MxFewArgs{a, nullptr, 0, 0}, stream);
+  if (a.blocks > 0 && a.a_stride <= kMostTileStride && a.b_stride <= kMostTileStride && a.a_scales_stride <= kMostTileStride && a.b_scales_stride <= kMostTileStride) {
     const u64 t4 = ((a.m + 255) / 256) * ((a.n + 255) / 256), t2 = ((a.m + 127) / 128) * ((a.n + 127) / 128), t1 = ((a.m + 63) / 64) * ((a.n + 63) / 64);
     if (t4 >= 200) launch_tiles<4>(a, stream);
     else if (t2 >= 200) launch_tiles<2>(a, stream);
@@ -235,13 +257,25 @@ int zc_mx_linear(const void* d_x, int x_type, size_t x_stride, const void* d_w, 
   if (!sizes_valid(n, k) || (flags & ~ZC_MX_ADD) || !matrix_valid(d_out, out_type, m, n, out_stride) || !aligned(d_bias, 4) ||
       !held_valid(d_w, d_w_scales, n, k, w_stride, w_scales_stride))
     return ZC_ERR_ARG;
-  if (n == 0) return ZC_OK;
-  if (k) {
-    const int st = zc_mx_quantize(d_x, x_type, m, k, x_stride, codes, codes_stride, scales, scales_stride, nullptr, 0, nullptr, 0, hip_stream);
-    if (st != ZC_OK) return st;
+  if (m == 0 || n == 0) return ZC_OK;
+  MxProductArgs a;
+  a.a = codes, a.a_scales = scales;
+  a.b = static_cast<const u8*>(d_w), a.b_scales = static_cast<const u8*>(d_w_scales);
+  a.a_stride = codes_stride, a.a_scales_stride = scales_stride, a.b_stride = w_stride, a.b_scales_stride = w_scales_stride;
+  a.m = m, a.n = n;
+  a.blocks = u32(num_blocks(k));
+  a.bias = d_bias;
+  a.out = d_out;
+  a.out_stride = out_stride;
+  a.out_type = out_type;
+  a.add = flags & ZC_MX_ADD;
+  hipStream_t const stream = static_cast<hipStream_t>(hip_stream);
+  if (m <= kFewRows) {
+    const MxFewArgs few{a, d_x, x_stride, k};
+    return x_type == ZC_F32 ? launch_few<ZC_F32>(few, stream) : x_type == ZC_BF16 ? launch_few<ZC_BF16>(few, stream) : launch_few<ZC_F16>(few, stream);
   }
-  return zc_mx_product(codes, codes_stride, scales, scales_stride, d_w, w_stride, d_w_scales, w_scales_stride, m, n, k, d_bias, d_out, out_type,
-                       out_stride, flags, nullptr, 0, hip_stream);
+  const int st = zc_mx_quantize(d_x, x_type, m, k, x_stride, codes, codes_stride, scales, scales_stride, nullptr, 0, nullptr, 0, hip_stream);
+  return st != ZC_OK ? st : product(a, stream);
 }
 
 }  // extern "C"
