@@ -18,7 +18,8 @@ namespace zc {
 constexpr int kAdamwThreads = 256;
 constexpr int kAdamwFours = 4;                                       // a lane's groups of four values
 constexpr u32 kAdamwTile = kAdamwThreads * 4 * kAdamwFours;
-constexpr int kAdamwTensors = 80;                                    // of one launch: their table travels in the kernel's arguments
+constexpr int kAdamwTensors = 110;                                   // of one launch: their table travels in the kernel's arguments
+constexpr u64 kAdamwMost = u64(1) << 31;                             // values of an entry: a longer tensor has several
 
 struct AdamwScalars {
   float b1, c1, b2, c2;          // c = 1 - b
@@ -28,17 +29,7 @@ struct AdamwScalars {
   float eps;
 };
 
-struct AdamwTensor {
-  void* param;
-  const void* grad;
-  void* copy;
-  u64 n;
-  u32 first_block;               // in the state
-};
-
 struct AdamwArgs {
-  u32 first_tile[kAdamwTensors];
-  AdamwTensor tensor[kAdamwTensors];
   AdamwScalars c;
   u32 tensors;
   int copy_type;
@@ -47,6 +38,12 @@ struct AdamwArgs {
   const float* grad_scale;
   u32 key;
   u32 stochastic;
+  u32 first_tile[kAdamwTensors];
+  u32 first_block[kAdamwTensors];          // in the state
+  u32 n[kAdamwTensors];
+  void* param[kAdamwTensors];
+  const void* grad[kAdamwTensors];
+  void* copy[kAdamwTensors];
 };
 static_assert(sizeof(AdamwArgs) <= 4096);
 
@@ -67,20 +64,6 @@ __host__ __device__ inline u64 adamw_second(u64 blocks, int bits) { return block
 __host__ __device__ inline u64 adamw_scales(u64 blocks) { return 2 * blocks * kBlockValues; }
 __host__ __device__ inline u64 adamw_bytes(u64 blocks, int bits) {
   return bits == 32 ? 2 * adamw_second(blocks, 32) : adamw_scales(blocks) + 2 * pad16(blocks);
-}
-
-template <int TYPE>
-__device__ inline void load_four(const void* base, u64 i, u64 n, float (&v)[4]) {
-  using One = typename ValueOf<TYPE>::One;
-  const One* const p = static_cast<const One*>(base) + i;
-  if (i + 4 <= n) {
-    const typename ValueOf<TYPE>::Four f = *reinterpret_cast<const typename ValueOf<TYPE>::Four*>(p);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = float(f.v[j]);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = i + j < n ? float(p[j]) : 0.0f;
-  }
 }
 
 // Largest magnitude as bits (every NaN counts as more than infinity): of a lane's four values, and of 8 neighbouring lanes, in pairs, in fours
@@ -124,92 +107,153 @@ __device__ inline void values_of_codes(u32 codes, float scale, float (&v)[4]) {
   v[3] = high[1] * scale;
 }
 
-template <int P, int G, int BITS>
-__global__ __launch_bounds__(kAdamwThreads) void adamw_kernel(AdamwArgs a) {
-  float scale = 1.0f;
-  if (a.grad_scale) {
-    scale = *a.grad_scale;
-    if (!(fabsf(scale) <= 3.402823466e38f)) return;                  // (not a number or infinite: no step)
+// Four values as they lie in memory, and as numbers.
+template <int TYPE>
+__device__ inline typename ValueOf<TYPE>::Four load_raw(const void* base, u32 i) {
+  using One = typename ValueOf<TYPE>::One;
+  return *reinterpret_cast<const typename ValueOf<TYPE>::Four*>(static_cast<const One*>(base) + i);
+}
+template <int TYPE>
+__device__ inline void load_some(const void* base, u32 i, u32 n, typename ValueOf<TYPE>::Four& to) {
+  using One = typename ValueOf<TYPE>::One;
+#pragma unroll
+  for (u32 j = 0; j < 4; ++j)
+    if (i + j < n) to.v[j] = static_cast<const One*>(base)[i + j];
+}
+
+// A state's share of a lane.
+template <int BITS> struct AdamwHeld;
+template <> struct AdamwHeld<32> {
+  f32x4_t m, v;
+  __device__ void load(const AdamwArgs& a, u64 at) {
+    m = *reinterpret_cast<const f32x4_t*>(a.state + 4 * at);
+    v = *reinterpret_cast<const f32x4_t*>(a.state + adamw_second(a.blocks, 32) + 4 * at);
   }
-  // The tensor that the workgroup's tile lies in: the last one that begins at or before it.
-  const u32 lane = threadIdx.x & 63u;
-  u32 t = 0;
-  for (u32 i = 0; i < a.tensors; i += 64)
-    t += u32(__popcll(__ballot(i + lane < a.tensors && a.first_tile[i + lane] <= blockIdx.x)));
-  t = u32(__builtin_amdgcn_readfirstlane(int(t))) - 1u;
-  const AdamwTensor x = a.tensor[t];
-  const u64 tile_at = u64(blockIdx.x - a.first_tile[t]) * kAdamwTile;
-  const u64 padded = num_blocks(x.n) * kBlockValues;
-  const u64 state_at = u64(x.first_block) * kBlockValues;
+};
+template <> struct AdamwHeld<8> {
+  u32 m, r, m_scale, r_scale;
+  __device__ void load(const AdamwArgs& a, u64 at) {
+    const u8* const scales = a.state + adamw_scales(a.blocks) + at / kBlockValues;
+    m = *reinterpret_cast<const u32*>(a.state + at);
+    r = *reinterpret_cast<const u32*>(a.state + adamw_second(a.blocks, 8) + at);
+    m_scale = scales[0];
+    r_scale = scales[pad16(a.blocks)];
+  }
+};
+
+struct AdamwEntry {
+  void* param;
+  const void* grad;
+  void* copy;
+  u32 n, tile_at;
+  u64 state_at;
+};
+
+// A workgroup's tile of an entry.  WHOLE: every value of it exists.  All loads come before the first use of one.
+template <int P, int G, int BITS, bool WHOLE>
+__device__ __forceinline__ void adamw_tile(const AdamwArgs& a, const AdamwEntry& x, float scale) {
   const AdamwScalars c = a.c;
+  const u32 padded = (x.n + kBlockValues - 1u) & ~u32(kBlockValues - 1);
+  typename ValueOf<P>::Four raw_p[kAdamwFours] = {};
+  typename ValueOf<G>::Four raw_g[kAdamwFours] = {};
+  AdamwHeld<BITS> held[kAdamwFours] = {};
 #pragma unroll
   for (int u = 0; u < kAdamwFours; ++u) {
-    const u64 i = tile_at + u64(u) * (kAdamwThreads * 4) + threadIdx.x * 4u;
-    const bool here = i < padded;
-    const u64 s = state_at + i, block = s / kBlockValues;
-    float p[4], g[4], m[4], v[4], r[4];
-    load_four<P>(x.param, i, x.n, p);
-    load_four<G>(x.grad, i, x.n, g);
-    if (BITS == 32) {
-      const float* const ms = reinterpret_cast<const float*>(a.state);
-      const float* const vs = reinterpret_cast<const float*>(a.state + adamw_second(a.blocks, 32));
+    const u32 i = x.tile_at + u32(u) * (kAdamwThreads * 4) + threadIdx.x * 4u;
+    if (WHOLE || i + 4 <= x.n) {
+      raw_p[u] = load_raw<P>(x.param, i);
+      raw_g[u] = load_raw<G>(x.grad, i);
+    }
+    if (WHOLE || i < padded) held[u].load(a, x.state_at + i);
+  }
+  if (!WHOLE && (x.n & 3u)) {                                        // (one lane of the last tile)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) m[j] = here ? ms[s + j] : 0.0f, v[j] = here ? vs[s + j] : 0.0f;
+    for (int u = 0; u < kAdamwFours; ++u) {
+      const u32 i = x.tile_at + u32(u) * (kAdamwThreads * 4) + threadIdx.x * 4u;
+      if (i < x.n && i + 4 > x.n) {
+        load_some<P>(x.param, i, x.n, raw_p[u]);
+        load_some<G>(x.grad, i, x.n, raw_g[u]);
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kAdamwFours; ++u) {
+    const u32 i = x.tile_at + u32(u) * (kAdamwThreads * 4) + threadIdx.x * 4u;
+    if (!WHOLE && x.tile_at + u32(u) * (kAdamwThreads * 4) >= padded) break;
+    const u64 s = x.state_at + i, block = s / kBlockValues;
+    float p[4], g[4], m[4], v[4], r[4];
+    if constexpr (BITS == 32) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m[j] = held[u].m[j], v[j] = held[u].v[j];
     } else {
-      const u8* const scales = a.state + adamw_scales(a.blocks);
-      const u32 mc = here ? *reinterpret_cast<const u32*>(a.state + s) : 0u;
-      const u32 rc = here ? *reinterpret_cast<const u32*>(a.state + adamw_second(a.blocks, 8) + s) : 0u;
-      values_of_codes(mc, scale_value(here ? scales[block] : 0u), m);
-      values_of_codes(rc, scale_value(here ? scales[pad16(a.blocks) + block] : 0u), v);
+      values_of_codes(held[u].m, scale_value(held[u].m_scale), m);
+      values_of_codes(held[u].r, scale_value(held[u].r_scale), v);
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] = v[j] * v[j];
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float gs = a.grad_scale ? g[j] * scale : g[j];
-      m[j] = m[j] * c.b1 + gs * c.c1;
-      v[j] = v[j] * c.b2 + (gs * c.c2) * gs;
+      p[j] = float(raw_p[u].v[j]);
+      g[j] = float(raw_g[u].v[j]);
+      if (a.grad_scale) g[j] = g[j] * scale;
+      m[j] = m[j] * c.b1 + g[j] * c.c1;
+      v[j] = v[j] * c.b2 + (g[j] * c.c2) * g[j];
       r[j] = sqrtf(v[j]);
       p[j] = p[j] * c.keep - (m[j] / (r[j] * c.root + c.eps)) * c.rate;
     }
-    if (i + 4 <= x.n) {
+    if (WHOLE || i + 4 <= x.n) {
       store_four<P>(x.param, i, p);
       if (x.copy) store_four(x.copy, a.copy_type, i, p);
-    } else {
-      for (int j = 0; j < 4; ++j)
+    } else if (i < x.n) {
+#pragma unroll
+      for (u32 j = 0; j < 4; ++j)
         if (i + j < x.n) {
           store_value(x.param, P, i + j, p[j]);
           if (x.copy) store_value(x.copy, a.copy_type, i + j, p[j]);
         }
     }
-    if (BITS == 32) {
-      float* const ms = reinterpret_cast<float*>(a.state);
-      float* const vs = reinterpret_cast<float*>(a.state + adamw_second(a.blocks, 32));
-      if (here) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) ms[s + j] = m[j], vs[s + j] = v[j];
+    if constexpr (BITS == 32) {
+      if (WHOLE || i < padded) {
+        *reinterpret_cast<f32x4_t*>(a.state + 4 * s) = f32x4_t{m[0], m[1], m[2], m[3]};
+        *reinterpret_cast<f32x4_t*>(a.state + adamw_second(a.blocks, 32) + 4 * s) = f32x4_t{v[0], v[1], v[2], v[3]};
       }
     } else {
-      u8* const scales = a.state + adamw_scales(a.blocks);
       const u32 sm = adamw_scale(top_of_eight(top_of_four(m))), sr = adamw_scale(top_of_eight(top_of_four(r)));
       float cm[4], cr[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const u32 z = mixed_word(u32(s + j) * 0x9E3779B1u + a.key);
+      for (u32 j = 0; j < 4; ++j) {
+        const u32 z = mixed_word((u32(s) + j) * 0x9E3779B1u + a.key);
         cm[j] = copysignf(on_grid(fabsf(m[j]) * power_of_two(254u - min(sm, 253u)), z & 0xffffu, a.stochastic), m[j]);
         cr[j] = on_grid(r[j] * power_of_two(254u - min(sr, 253u)), z >> 16, a.stochastic);
         if (r[j] > 0.0f) cr[j] = fmaxf(cr[j], 0x1p-9f);              // (a denominator never becomes none)
       }
-      if (here) {
+      if (WHOLE || i < padded) {
+        u8* const scales = a.state + adamw_scales(a.blocks) + block;
         *reinterpret_cast<u32*>(a.state + s) = sm == 255u ? 0u : four_codes(cm);
         *reinterpret_cast<u32*>(a.state + adamw_second(a.blocks, 8) + s) = sr == 255u ? 0u : four_codes(cr);
-        if ((lane & 7u) == 0) {
-          scales[block] = u8(sm);
-          scales[pad16(a.blocks) + block] = u8(sr);
+        if ((threadIdx.x & 7u) == 0) {
+          scales[0] = u8(sm);
+          scales[pad16(a.blocks)] = u8(sr);
         }
       }
     }
   }
+}
+
+template <int P, int G, int BITS>
+__global__ __launch_bounds__(kAdamwThreads) void adamw_kernel(AdamwArgs a) {
+  float scale = 1.0f;
+  if (a.grad_scale) scale = *a.grad_scale;
+  // The entry that the workgroup's tile lies in: the last one that begins at or before it.
+  const u32 lane = threadIdx.x & 63u;
+  u32 t = 0;
+  for (u32 i = 0; i < a.tensors; i += 64)
+    t += u32(__popcll(__ballot(i + lane < a.tensors && a.first_tile[i + lane] <= blockIdx.x)));
+  t = u32(__builtin_amdgcn_readfirstlane(int(t))) - 1u;
+  if (!(fabsf(scale) <= 3.402823466e38f)) return;                    // (not a number or infinite: no step)
+  const AdamwEntry x = {a.param[t], a.grad[t], a.copy[t], a.n[t], (blockIdx.x - a.first_tile[t]) * kAdamwTile, u64(a.first_block[t]) * kBlockValues};
+  if (x.tile_at + kAdamwTile <= x.n) adamw_tile<P, G, BITS, true>(a, x, scale);
+  else adamw_tile<P, G, BITS, false>(a, x, scale);
 }
 
 }  // namespace zc

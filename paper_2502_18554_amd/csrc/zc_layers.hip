@@ -168,13 +168,20 @@ int zc_adamw(int k, const size_t* n, void* const* d_params, int param_type, cons
     a.tensors = tiles = 0;
   };
   for (int i = 0; i < k; ++i) {
-    if (n[i] == 0) continue;
-    const u64 own = (n[i] + kAdamwTile - 1) / kAdamwTile;
-    if (a.tensors == kAdamwTensors || tiles + own > kMostGroups) go();
-    a.first_tile[a.tensors] = tiles;
-    a.tensor[a.tensors++] = {d_params[i], d_grads[i], d_copies ? d_copies[i] : nullptr, n[i], u32(block)};
-    tiles += u32(own);
-    block += num_blocks(n[i]);
+    for (u64 at = 0; at < n[i]; at += kAdamwMost) {
+      const u64 now = n[i] - at < kAdamwMost ? n[i] - at : kAdamwMost;
+      const u32 own = u32((now + kAdamwTile - 1) / kAdamwTile);
+      if (a.tensors == kAdamwTensors || u64(tiles) + own > kMostGroups) go();
+      a.first_tile[a.tensors] = tiles;
+      a.first_block[a.tensors] = u32(block);
+      a.n[a.tensors] = u32(now);
+      a.param[a.tensors] = static_cast<u8*>(d_params[i]) + at * value_bytes(param_type);
+      a.grad[a.tensors] = static_cast<const u8*>(d_grads[i]) + at * value_bytes(grad_type);
+      a.copy[a.tensors] = d_copies && d_copies[i] ? static_cast<u8*>(d_copies[i]) + at * value_bytes(copy_type) : nullptr;
+      ++a.tensors;
+      tiles += own;
+      block += num_blocks(now);
+    }
   }
   if (a.tensors) go();
   return launched();
