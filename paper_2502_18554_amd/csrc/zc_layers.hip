@@ -56,10 +56,11 @@ bool matrix_valid(const void* p, int type, u64 rows, u64 cols, u64 stride) {
 }
 bool sizes_valid(u64 rows, u64 cols) { return rows <= 0x7fffffffu && cols <= 0x7fffffffu; }
 
-template <int T>
+template <int T, int TYPE>
 void launch_tiles(const MxProductArgs& a, hipStream_t stream) {
   const u64 down = (a.m + mx_tile_rows(T) - 1) / mx_tile_rows(T), across = (a.n + mx_tile_rows(T) - 1) / mx_tile_rows(T);
-  hipLaunchKernelGGL((mx_tile_kernel<T, T>), dim3(u32(down * across)), dim3(256), 0, stream, a, u32(down), u32(across));
+  const u64 at_once = 256 * (T == 4 ? 1 : T == 2 ? 2 : 4);            // workgroups that the GPU holds
+  hipLaunchKernelGGL((mx_tile_kernel<T, T, TYPE>), dim3(u32(down * across < at_once ? down * across : at_once)), dim3(256), 0, stream, a, u32(down), u32(across));
 }
 
 // Few rows: as many columns a workgroup as leave a workgroup for every CU.
@@ -80,6 +81,13 @@ int launch_few(const MxFewArgs& a, hipStream_t stream) {
   if (a.p.m <= 16) launch_few<1, X>(a, stream);
   else launch_few<2, X>(a, stream);
   return launched();
+}
+
+template <int T>
+void launch_tiles(const MxProductArgs& a, hipStream_t stream) {
+  if (a.out_type == ZC_F32) launch_tiles<T, ZC_F32>(a, stream);
+  else if (a.out_type == ZC_BF16) launch_tiles<T, ZC_BF16>(a, stream);
+  else launch_tiles<T, ZC_F16>(a, stream);
 }
 
 int product(const MxProductArgs& a, hipStream_t stream) {
