@@ -117,52 +117,89 @@ __device__ inline const __attribute__((address_space(3))) T* mx_lds(u32 at) {
   return reinterpret_cast<const __attribute__((address_space(3))) T*>(at);
 }
 
-// A lane's results: of rows row0 + 32 i, 16 neighbouring ones from column col0 + 32 j on.
-template <int TM, int TN, int TYPE>
-__device__ __forceinline__ void mx_write_tile(const MxProductArgs& a, u64 row0, u64 col0, f32x16_t (&sum)[TM][TN]) {
+// Between two registers: 16 lanes 1 and 3 (of 0 .. 3) of the first with 16 lanes 0 and 2 of the second; the upper half of the first with the lower half of the second.
+__device__ inline void swap_sixteens(u32& a, u32& b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  a = r[0], b = r[1];
+}
+__device__ inline void swap_halves(u32& a, u32& b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = r[0], b = r[1];
+}
+
+// Two neighbouring values of a type, rounded, as a word; a value of 32 bits is one.
+template <int TYPE>
+__device__ inline u32 packed_pair(float low, float high) {
+  typedef float Two __attribute__((ext_vector_type(2)));
+  typedef typename ValueOf<TYPE>::One Pair __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(u32, __builtin_convertvector((Two{low, high}), Pair));
+}
+
+// The results of a wave: row0 and col0 are its tile's first.  Lane l has, of 32 x 32, 16 neighbouring ones of row l % 32, from column 16 (l / 32) on.  Its pieces of 16 bytes go to
+// other lanes so that four lanes write 64 bytes of a row together (16 rows a store): single pieces would be that many more requests to L2.
+// WHOLE: the matrix has all of these results.
+template <int TM, int TN, int TYPE, bool WHOLE>
+__device__ __forceinline__ void mx_write_tile(const MxProductArgs& a, u64 row0, u64 col0, u32 lane, f32x16_t (&sum)[TM][TN]) {
   using One = typename ValueOf<TYPE>::One;
-  constexpr u32 N = 16 / sizeof(One);                   // values of a store
-  typedef One Sixteen __attribute__((ext_vector_type(N)));
-  struct __attribute__((packed, aligned(2))) Stored { Sixteen v; };
+  constexpr u32 N = 16 / sizeof(One), PIECES = 16 / N;   // values of a piece; a lane's pieces
+  struct __attribute__((packed, aligned(2))) Piece { u32 w[4]; };
+  const u64 own_row0 = row0 + (lane & 31u), own_col0 = col0 + 16 * (lane >> 5);
+  const u64 to_row0 = row0 + (lane & 15u), to_col0 = col0 + N * (lane >> 4);
+  One* const to0 = static_cast<One*>(a.out) + to_row0 * a.out_stride + to_col0;
 #pragma unroll
   for (int j = 0; j < TN; ++j) {
-    const u64 col = col0 + 32 * j;
-    const bool whole = col + 16 <= a.n;
+    const u64 own_col = own_col0 + 32 * j;
     float bias[16];
     if (a.bias) {
 #pragma unroll
-      for (u32 c = 0; c < 16; ++c) bias[c] = col + c < a.n ? a.bias[col + c] : 0.0f;
+      for (u32 c = 0; c < 16; ++c) bias[c] = WHOLE || own_col + c < a.n ? a.bias[own_col + c] : 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       asm volatile("" : "+a"(sum[i][j]));                // (leaves the results in their registers until they are wanted)
-      const u64 row = row0 + 32 * i;
-      if (row >= a.m) continue;
-      One* const out = static_cast<One*>(a.out) + row * a.out_stride + col;
+      float v[16];
 #pragma unroll
-      for (u32 q = 0; q < 16 / N; ++q) {
-        float v[N];
+      for (u32 c = 0; c < 16; ++c) v[c] = sum[i][j][c];
+      if (a.bias) {
 #pragma unroll
-        for (u32 c = 0; c < N; ++c) v[c] = sum[i][j][N * q + c];
-        if (a.bias) {
+        for (u32 c = 0; c < 16; ++c) v[c] += bias[c];
+      }
+      const u64 own_row = own_row0 + 32 * i;
+      if (a.add && (WHOLE || own_row < a.m)) {
+        const One* const before = static_cast<const One*>(a.out) + own_row * a.out_stride + own_col;
 #pragma unroll
-          for (u32 c = 0; c < N; ++c) v[c] += bias[N * q + c];
+        for (u32 c = 0; c < 16; ++c)
+          if (WHOLE || own_col + c < a.n) v[c] += float(before[c]);
+      }
+      u32 w[PIECES][4];
+#pragma unroll
+      for (u32 d = 0; d < 4 * PIECES; ++d) {
+        if constexpr (TYPE == ZC_F32) w[d / 4][d % 4] = __float_as_uint(v[d]);
+        else w[d / 4][d % 4] = packed_pair<TYPE>(v[2 * d], v[2 * d + 1]);
+      }
+#pragma unroll
+      for (u32 d = 0; d < 4; ++d) {
+        if constexpr (PIECES == 4) {
+          swap_halves(w[0][d], w[2][d]);
+          swap_halves(w[1][d], w[3][d]);
+          swap_sixteens(w[2][d], w[3][d]);
         }
-        if (whole) {
-          Stored* const to = reinterpret_cast<Stored*>(out + N * q);
-          if (a.add) {
-            const Stored before = *to;
+        swap_sixteens(w[0][d], w[1][d]);
+      }
+      // Piece q of a lane is now: row 16 (q % 2) + l % 16, 64 bytes number q / 2, of those the 16 bytes l / 16.
 #pragma unroll
-            for (u32 c = 0; c < N; ++c) v[c] += float(before.v[c]);
-          }
-          Stored s;
-#pragma unroll
-          for (u32 c = 0; c < N; ++c) s.v[c] = One(v[c]);
-          *to = s;
-        } else {
+      for (u32 q = 0; q < PIECES; ++q) {
+        One* const to = to0 + (32 * i + 16 * (q & 1u)) * a.out_stride + (32 * j + 4 * N * (q / 2));
+        const u64 row = to_row0 + 32 * i + 16 * (q & 1u), col = to_col0 + 32 * j + 4 * N * (q / 2);
+        if (WHOLE || (row < a.m && col + N <= a.n)) {
+          *reinterpret_cast<Piece*>(to) = Piece{{w[q][0], w[q][1], w[q][2], w[q][3]}};
+        } else if (row < a.m && col < a.n) {
+          asm volatile("" ::: "memory");                 // (keeps the stores above in one piece)
+          One piece[N];
+          __builtin_memcpy(piece, w[q], 16);
 #pragma unroll
           for (u32 c = 0; c < N; ++c)
-            if (col + N * q + c < a.n) out[N * q + c] = One(a.add ? v[c] + float(out[N * q + c]) : v[c]);
+            if (col + c < a.n) to[c] = piece[c];
         }
       }
     }
@@ -346,8 +383,9 @@ __global__ __launch_bounds__(256, TM * TN > 4 ? 1 : 2) void mx_tile_kernel(MxPro
     }
     u32 down, across;
     tiles.place(tile, down, across);
-    const u64 row0 = u64(down) * RA + wave_a + in32, col0 = u64(across) * RB + wave_b + 16 * half;
-    mx_write_tile<TM, TN, TYPE>(a, row0, col0, sum);
+    const u64 row0 = u64(down) * RA + wave_a, col0 = u64(across) * RB + wave_b;
+    if (row0 + 32 * TM <= a.m && col0 + 32 * TN <= a.n) mx_write_tile<TM, TN, TYPE, true>(a, row0, col0, lane, sum);
+    else mx_write_tile<TM, TN, TYPE, false>(a, row0, col0, lane, sum);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (the last requests, too, before the workgroup's LDS is given to another one)
 }
