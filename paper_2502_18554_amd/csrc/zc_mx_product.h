@@ -54,7 +54,7 @@ __device__ inline void mx_finish(const MxProductArgs& a, u64 row, u64 col, float
 //
 // A stage is 8 blocks (128 bytes) of every row of the tile, brought straight to LDS while the stage before is multiplied.  Rows follow each
 // other in LDS, their eight 16-byte blocks exchanged by the row's number, so that 16 lanes that read LDS together find 64 different banks.
-// Scale bytes come by two stages (16 bytes of a row) through registers.
+// Scale bytes come by four stages (32 bytes of a row, by two lanes) through registers.
 //
 // An instruction multiplies two blocks of 32 rows with 32 columns: lanes 0 .. 31 bring one block each, lanes 32 .. 63 the other.  Which two blocks of the
 // stage these are is free: it is blocks t and 4 + t, so that a lane's scale bytes of the stage are the four bytes of one word, of which
@@ -209,9 +209,9 @@ __device__ __forceinline__ void mx_write_tile(const MxProductArgs& a, u64 row0, 
 template <int TM, int TN, int TYPE>
 __global__ __launch_bounds__(256, TM * TN > 4 ? 1 : 2) void mx_tile_kernel(MxProductArgs a, u32 tiles_down, u32 tiles_across) {
   constexpr u32 RA = mx_tile_rows(TM), RB = mx_tile_rows(TN), ROWS = RA + RB, LOADS = ROWS / 32;
-  constexpr u32 SCALE_ROWS = (ROWS + 255) / 256;
-  // In LDS: two stages of a's rows, two of b's, the scale bytes of two pairs of stages of a's rows, of b's.
-  constexpr u32 AT_B = 2 * RA * 128, AT_SCALES_A = 2 * ROWS * 128, AT_SCALES_B = AT_SCALES_A + 2 * RA * 16, LDS_BYTES = AT_SCALES_B + 2 * RB * 16;
+  constexpr u32 SCALE_LOADS = ROWS / 128;
+  // In LDS: two stages of a's rows, two of b's, the scale bytes of four pairs of stages of a's rows, of b's.
+  constexpr u32 AT_B = 2 * RA * 128, AT_SCALES_A = 2 * ROWS * 128, AT_SCALES_B = AT_SCALES_A + 4 * RA * 16, LDS_BYTES = AT_SCALES_B + 4 * RB * 16;
   __shared__ u32x4_t memory[LDS_BYTES / 16];
   const u32 tid = threadIdx.x, lane = tid & 63u, wave = u32(__builtin_amdgcn_readfirstlane(int(tid >> 6)));
   const u32 half = lane >> 5, in32 = lane & 31u;
@@ -263,35 +263,33 @@ __global__ __launch_bounds__(256, TM * TN > 4 ? 1 : 2) void mx_tile_kernel(MxPro
     rows_a.move_on(128);
     rows_b.move_on(128);
   };
-  u32x4_t held[SCALE_ROWS];
-  const auto ask_scales = [&] {                         // 16 scale bytes of a row, those behind the last block as zeros
+  u32x4_t held[SCALE_LOADS];
+  const auto ask_scales = [&] {                         // 16 scale bytes of a row for the pair that is asked for, 16 for the next one; those behind the last block as zeros
 #pragma unroll
-    for (u32 i = 0; i < SCALE_ROWS; ++i) {
-      if (64 * wave + 256 * i >= ROWS) continue;
-      const bool of_a = 64 * wave + 256 * i < RA;
-      const u32 at = of_a ? (tid + 256 * i) * u32(a.a_scales_stride) : (tid + 256 * i - RA) * u32(a.b_scales_stride);
-      if (16 * ask_pair + 16 <= a.blocks) {
-        held[i] = of_a ? __builtin_amdgcn_raw_buffer_load_b128(scales_a.buffer(), at, 0, 0) : __builtin_amdgcn_raw_buffer_load_b128(scales_b.buffer(), at, 0, 0);
+    for (u32 i = 0; i < SCALE_LOADS; ++i) {
+      const u32 row = (tid >> 1) + 128 * i;
+      const bool of_a = 32 * wave + 128 * i < RA;
+      const u32 at = (of_a ? row * u32(a.a_scales_stride) : (row - RA) * u32(a.b_scales_stride)) + 16 * (tid & 1u);
+      const __amdgpu_buffer_rsrc_t from = of_a ? scales_a.buffer() : scales_b.buffer();
+      if (16 * ask_pair + 32 <= a.blocks) {
+        held[i] = __builtin_amdgcn_raw_buffer_load_b128(from, at, 0, 0);
       } else {
-        u32x4_t w = {0, 0, 0, 0};
 #pragma unroll
         for (u32 j = 0; j < 4; ++j) {
-          const u32 first = 16 * ask_pair + 4 * j;
-          if (first >= a.blocks) continue;
-          w[j] = of_a ? __builtin_amdgcn_raw_buffer_load_b32(scales_a.buffer(), at + 4 * j, 0, 0) : __builtin_amdgcn_raw_buffer_load_b32(scales_b.buffer(), at + 4 * j, 0, 0);
-          if (first + 4 > a.blocks) w[j] &= (1u << (8 * (a.blocks - first))) - 1u;
+          const u32 first = 16 * (ask_pair + (tid & 1u)) + 4 * j;
+          const u32 w = __builtin_amdgcn_raw_buffer_load_b32(from, first < a.blocks ? at + 4 * j : ~0u, 0, 0);
+          held[i][j] = first + 4 <= a.blocks || first >= a.blocks ? w : w & ((1u << (8 * (a.blocks - first))) - 1u);
         }
-        held[i] = w;
       }
     }
   };
-  const auto put_scales = [&](u32 parity) {
+  const auto put_scales = [&](u32 plane) {              // into this plane and the next one
 #pragma unroll
-    for (u32 i = 0; i < SCALE_ROWS; ++i)
-      if (64 * wave + 256 * i < ROWS) {
-        const bool of_a = 64 * wave + 256 * i < RA;
-        memory[(of_a ? AT_SCALES_A : AT_SCALES_B - RA * 16) / 16 + parity * (of_a ? RA : RB) + tid + 256 * i] = held[i];
-      }
+    for (u32 i = 0; i < SCALE_LOADS; ++i) {
+      const u32 row = (tid >> 1) + 128 * i;
+      const bool of_a = 32 * wave + 128 * i < RA;
+      memory[(of_a ? AT_SCALES_A : AT_SCALES_B - RA * 16) / 16 + (plane + (tid & 1u)) * (of_a ? RA : RB) + row] = held[i];
+    }
   };
 
   const u32 wave_a = (wave >> 1) * 32u * TM, wave_b = (wave & 1u) * 32u * TN;
@@ -309,9 +307,9 @@ __global__ __launch_bounds__(256, TM * TN > 4 ? 1 : 2) void mx_tile_kernel(MxPro
     if (i < TM) fa[t & 1][i] = *mx_lds<u32x4_t>(at_a[t] + (buffer * RA * 128u + 4096u * i));
     else fb[t & 1][i - TM] = *mx_lds<u32x4_t>(at_b[t] + (buffer * RB * 128u + 4096u * (i - TM)));
   };
-  const auto read_scales = [&](u32 parity, u32 u, u32 i) {
-    if (i < TM) sa[u][i] = *mx_lds<u32>(at_sa + parity * (RA * 16u) + (8 * u + 512u * i));
-    else sb[u][i - TM] = *mx_lds<u32>(at_sb + parity * (RB * 16u) + (8 * u + 512u * (i - TM)));
+  const auto read_scales = [&](u32 plane, u32 u, u32 i) {
+    if (i < TM) sa[u][i] = *mx_lds<u32>(at_sa + plane * (RA * 16u) + (8 * u + 512u * i));
+    else sb[u][i - TM] = *mx_lds<u32>(at_sb + plane * (RB * 16u) + (8 * u + 512u * (i - TM)));
   };
 
   // The instructions of a step and what goes between them: in the first half the reads for the next step, and from the last step of a stage on, when its
@@ -330,7 +328,7 @@ __global__ __launch_bounds__(256, TM * TN > 4 ? 1 : 2) void mx_tile_kernel(MxPro
   for (u32 i = 0; i < EARLY; ++i) ask(1, i);
 #pragma unroll
   for (u32 i = 0; i < READS; ++i) read(0, 0, i), read_scales(0, 0, i);
-  u32 parity = 0;                                       // of the pairs, through all tiles
+  u32 plane = 0;                                        // of the four with scale bytes: the pair's
   for (u32 tile = tiles.first; tile < tiles.count; tile += tiles.step) {
     f32x16_t sum[TM][TN];
 #pragma unroll
@@ -340,12 +338,14 @@ __global__ __launch_bounds__(256, TM * TN > 4 ? 1 : 2) void mx_tile_kernel(MxPro
 #pragma unroll
         for (int r = 0; r < 16; ++r) sum[i][j][r] = 0.0f;
     for (u32 pair = 0; pair < pairs; ++pair) {
+      const u32 next_plane = (pair & 1u) == 0 && pair + 1 < pairs ? plane + 1u : (plane & 2u) ^ 2u;
+      const bool fresh = (next_plane & 1u) == 0;        // the scale bytes of the next two pairs are asked for during this one
 #pragma unroll
       for (u32 u = 0; u < 2; ++u) {
 #pragma unroll
         for (u32 t = 0; t < 4; ++t) {
           if (t == 3) {
-            if (u == 1) put_scales(parity ^ 1u);
+            if (u == 1 && fresh) put_scales(next_plane);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
           }
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(256, TM * TN > 4 ? 1 : 2) void mx_tile_kernel(MxPro
 #pragma unroll
             for (u32 i = 0; i < READS; ++i) {
               if (i * SLOTS / (2 * READS) == slot) read(t < 3 ? u : u ^ 1, (t + 1) & 3u, i);
-              if (t == 3 && SLOTS / 2 + i * SLOTS / (2 * READS) == slot) read_scales(u ? parity ^ 1u : parity, u ^ 1, i);
+              if (t == 3 && SLOTS / 2 + i * SLOTS / (2 * READS) == slot) read_scales(u ? next_plane : plane, u ^ 1, i);
             }
             const u32 i = slot / TN, j = slot % TN;
             const i32x8_t b = mx_operand(fb[t & 1][j]), x = mx_operand(fa[t & 1][i]);
@@ -375,11 +375,11 @@ __global__ __launch_bounds__(256, TM * TN > 4 ? 1 : 2) void mx_tile_kernel(MxPro
           if (t == 0) next_stage();
           if (u == 0 && t == 0) {
             next_pair();
-            ask_scales();
+            if (fresh) ask_scales();
           }
         }
       }
-      parity ^= 1u;
+      plane = next_plane;
     }
     u32 down, across;
     tiles.place(tile, down, across);
