@@ -229,8 +229,8 @@ __device__ __forceinline__ void adamw_tile(const AdamwArgs& a, const AdamwEntry&
       }
       if (WHOLE || i < padded) {
         u8* const scales = a.state + adamw_scales(a.blocks) + block;
-        *reinterpret_cast<u32*>(a.state + s) = sm == 255u ? 0u : four_codes(cm);
-        *reinterpret_cast<u32*>(a.state + adamw_second(a.blocks, 8) + s) = sr == 255u ? 0u : four_codes(cr);
+        *reinterpret_cast<u32*>(a.state + s) = codes_if(sm, four_codes(cm));
+        *reinterpret_cast<u32*>(a.state + adamw_second(a.blocks, 8) + s) = codes_if(sr, four_codes(cr));
         if ((threadIdx.x & 7u) == 0) {
           scales[0] = u8(sm);
           scales[pad16(a.blocks)] = u8(sr);

@@ -65,22 +65,23 @@ void launch_tiles(const MxProductArgs& a, hipStream_t stream) {
 
 // Few rows: as many columns a workgroup as leave a workgroup for every CU.
 template <int RG, int CG, int X>
-void launch_few(const MxFewArgs& a, hipStream_t stream) {
-  const u64 groups = (a.p.n + 16 * CG - 1) / (16 * CG), spans = (a.p.blocks + kSpanOfBlocks - 1) / kSpanOfBlocks;
-  const u32 waves = spans < 1 ? 1u : spans < kFewWaves ? u32(spans) : kFewWaves;
-  hipLaunchKernelGGL((mx_few_kernel<RG, CG, X>), dim3(u32(groups)), dim3(64 * waves), 0, stream, a);
+int launch_few(MxFewArgs a, hipStream_t stream) {
+  const u64 groups = (a.p.n + 16 * CG - 1) / (16 * CG), steps = (a.p.blocks + 3) / 4;
+  a.steps = steps >= 4 * kFewWaves ? 4 : steps >= 2 * kFewWaves ? 2 : 1;
+  const bool whole = a.steps == 4 && a.p.blocks % kSpanOfBlocks == 0 && (X == kHeldRows || a.k % kBlockValues == 0);
+  if (whole) hipLaunchKernelGGL((mx_few_kernel<RG, CG, X, true>), dim3(u32(groups)), dim3(64 * kFewWaves), 0, stream, a);
+  else hipLaunchKernelGGL((mx_few_kernel<RG, CG, X, false>), dim3(u32(groups)), dim3(64 * kFewWaves), 0, stream, a);
+  return launched();
 }
 template <int RG, int X>
-void launch_few(const MxFewArgs& a, hipStream_t stream) {
-  if (a.p.n >= 4 * 16 * 256) launch_few<RG, 4, X>(a, stream);
-  else if (a.p.n >= 2 * 16 * 256) launch_few<RG, 2, X>(a, stream);
-  else launch_few<RG, 1, X>(a, stream);
+int launch_few(const MxFewArgs& a, hipStream_t stream) {
+  if (a.p.n >= 4 * 16 * 256) return launch_few<RG, 4, X>(a, stream);
+  if (a.p.n >= 2 * 16 * 256) return launch_few<RG, 2, X>(a, stream);
+  return launch_few<RG, 1, X>(a, stream);
 }
 template <int X>
 int launch_few(const MxFewArgs& a, hipStream_t stream) {
-  if (a.p.m <= 16) launch_few<1, X>(a, stream);
-  else launch_few<2, X>(a, stream);
-  return launched();
+  return a.p.m <= 16 ? launch_few<1, X>(a, stream) : launch_few<2, X>(a, stream);
 }
 
 template <int T>
@@ -92,7 +93,7 @@ void launch_tiles(const MxProductArgs& a, hipStream_t stream) {
 
 int product(const MxProductArgs& a, hipStream_t stream) {
   if (a.m == 0 || a.n == 0) return ZC_OK;
-  if (a.m <= kFewRows) return launch_few<kHeldRows>(MxFewArgs{a, nullptr, 0, 0}, stream);
+  if (a.m <= kFewRows) return launch_few<kHeldRows>(MxFewArgs{a, nullptr, 0, 0, 0}, stream);
   if (a.blocks > 0 && a.a_stride <= kMostTileStride && a.b_stride <= kMostTileStride && a.a_scales_stride <= kMostTileStride && a.b_scales_stride <= kMostTileStride) {
     const u64 t4 = ((a.m + 255) / 256) * ((a.n + 255) / 256), t2 = ((a.m + 127) / 128) * ((a.n + 127) / 128), t1 = ((a.m + 63) / 64) * ((a.n + 63) / 64);
     if (t4 >= 200) launch_tiles<4>(a, stream);
@@ -285,8 +286,8 @@ int zc_mx_linear(const void* d_x, int x_type, size_t x_stride, const void* d_w, 
   a.out_type = out_type;
   a.add = flags & ZC_MX_ADD;
   hipStream_t const stream = static_cast<hipStream_t>(hip_stream);
-  if (m <= kFewRows) {
-    const MxFewArgs few{a, d_x, x_stride, k};
+  if (m <= kFewRows && x_stride <= kMostFewStride) {
+    const MxFewArgs few{a, d_x, x_stride, k, 0};
     return x_type == ZC_F32 ? launch_few<ZC_F32>(few, stream) : x_type == ZC_BF16 ? launch_few<ZC_BF16>(few, stream) : launch_few<ZC_F16>(few, stream);
   }
   const int st = zc_mx_quantize(d_x, x_type, m, k, x_stride, codes, codes_stride, scales, scales_stride, nullptr, 0, nullptr, 0, hip_stream);

@@ -144,16 +144,16 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 
       top = max(top, u32(__builtin_amdgcn_update_dpp(0, int(top), 0xB1, 0xf, 0xf, true)));                    // quad_perm 1 0 3 2
       if (LANES == 4) top = max(top, u32(__builtin_amdgcn_update_dpp(0, int(top), 0x4E, 0xf, 0xf, true)));    // quad_perm 2 3 0 1
       const u32 s = mx_scale(top);
-      const float scale = scale_value(s);
+      const float scale = divisor_value(s);
       const u64 block = col / kBlockValues;
       if (row < a.rows && block * kBlockValues < a.cols) {
         u8* const codes = a.held.codes + row * a.held.codes_stride + col / 2;
         if constexpr (TYPE == ZC_F32) {
           const u32 eight[8] = {w[0][0], w[0][1], w[0][2], w[0][3], w[1][0], w[1][1], w[1][2], w[1][3]};
-          *reinterpret_cast<u32*>(codes) = s == 255u ? 0u : mx_codes<TYPE>(eight, scale);
+          *reinterpret_cast<u32*>(codes) = codes_if(s, mx_codes<TYPE>(eight, scale));
         } else {
           const u32 low[4] = {w[0][0], w[0][1], w[0][2], w[0][3]}, high[4] = {w[1][0], w[1][1], w[1][2], w[1][3]};
-          *reinterpret_cast<u32x2_t*>(codes) = s == 255u ? u32x2_t{0, 0} : u32x2_t{mx_codes<TYPE>(low, scale), mx_codes<TYPE>(high, scale)};
+          *reinterpret_cast<u32x2_t*>(codes) = u32x2_t{codes_if(s, mx_codes<TYPE>(low, scale)), codes_if(s, mx_codes<TYPE>(high, scale))};
         }
         if (part % LANES == 0) a.held.scales[row * a.held.scales_stride + block] = u8(s);
       }
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 
     const u64 c = col0 + (TYPE == ZC_F32 ? lane : 2 * lane + h);
     if (c >= a.cols) break;
     const u32 s = mx_scale(TYPE == ZC_F32 ? top : Pack::top_value(h ? top >> 16 : top & 0xffffu));
-    const float scale = scale_value(s);
+    const float scale = divisor_value(s);
     u32x4_t codes;
 #pragma unroll
     for (u32 q = 0; q < 4; ++q) {
@@ -191,7 +191,8 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 
         codes[q] = mx_codes<TYPE>(four, scale);
       }
     }
-    if (s == 255u) codes = u32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (u32 q = 0; q < 4; ++q) codes[q] = codes_if(s, codes[q]);
     *reinterpret_cast<u32x4_t*>(a.held_t.codes + c * a.held_t.codes_stride + kMxBytes * block) = codes;
     a.held_t.scales[c * a.held_t.scales_stride + block] = u8(s);
   }

@@ -47,9 +47,13 @@ __device__ inline void store_four(void* base, int type, u64 i, const float (&v)[
 __device__ inline float power_of_two(u32 exponent) { return __uint_as_float(exponent << 23); }
 __device__ inline u32 exponent_field(float magnitude) { return __float_as_uint(magnitude) >> 23; }
 
-// What a scale byte stands for: 2^(s - 127), not a number for 255.
+// What a scale byte stands for: 2^(s - 127), not a number for 255.  (Written so that it takes no branch.)
 __device__ inline float scale_value(u32 s) {
-  return s == 255u ? __uint_as_float(0x7fc00000u) : s ? power_of_two(s) : __uint_as_float(0x00400000u);
+  const u32 bits = max(s << 23, 0x00400000u);
+  return __uint_as_float(s == 255u ? 0x7fc00000u : bits);
 }
+// Of a block that has a scale: what its values are divided by.  (Of one that has none anything: its codes are zeros, see codes_if.)
+__device__ inline float divisor_value(u32 s) { return __uint_as_float(max(s << 23, 0x00400000u)); }
+__device__ inline u32 codes_if(u32 s, u32 codes) { return codes & (s == 255u ? 0u : ~0u); }
 
 }  // namespace zc
