@@ -102,57 +102,61 @@ __host__ __device__ constexpr u32 mx_tile_cols(int type) { return kMxTileBytes /
 
 struct __attribute__((packed, aligned(2))) MxSixteen { u32 w[4]; };
 
-template <int TYPE, bool ALONG, bool DOWN>
-__global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 tiles_down, u32 tiles) {
+// WHOLE: the matrix has all of the tile; then nothing is asked about between the loads, and all of them are on their way together.
+template <int TYPE, bool ALONG, bool DOWN, bool WHOLE>
+__device__ __forceinline__ void mx_quantize_tile(const MxQuantizeArgs& a, u64 row0, u64 col0, u32x4_t* tile) {
   using One = typename ValueOf<TYPE>::One;
   using Pack = MxPack<TYPE>;
-  constexpr u32 N = 2 * Pack::kValues, COLS = mx_tile_cols(TYPE), LANES = kBlockValues / N;       // values of a thread, of a row; threads of a block
-  __shared__ u32x4_t tile[DOWN ? kMxTileRows * kMxTileBytes / 16 : 1];
+  constexpr u32 N = 2 * Pack::kValues, LANES = kBlockValues / N;          // values of a thread, of a row; threads of a block
   const u32 tid = threadIdx.x, part = tid & 7u;
-  const u32 xcd = blockIdx.x & 7u, t = xcd * (tiles >> 3) + min(xcd, tiles & 7u) + (blockIdx.x >> 3);
-  const u32 across = t / tiles_down;
-  const u64 row0 = u64(t - across * tiles_down) * kMxTileRows, col0 = u64(across) * COLS;
   const u64 col = col0 + part * N;
+  u32x4_t w[4][2];
 #pragma unroll
   for (u32 i = 0; i < 4; ++i) {
-    const u32 in_tile = 32 * i + (tid >> 3);
-    const u64 row = row0 + in_tile;
-    u32x4_t w[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    if (row < a.rows) {
-      const One* const p = static_cast<const One*>(a.in) + row * a.stride + col;
-      if (col + N <= a.cols) {
+    const u64 row = row0 + 32 * i + (tid >> 3);
+    const One* const p = static_cast<const One*>(a.in) + row * a.stride + col;
+    if (WHOLE || (row < a.rows && col + N <= a.cols)) {
 #pragma unroll
-        for (u32 h = 0; h < 2; ++h) {
-          const MxSixteen s = reinterpret_cast<const MxSixteen*>(p)[h];
-          w[h] = u32x4_t{s.w[0], s.w[1], s.w[2], s.w[3]};
-        }
-      } else if (col < a.cols) {
+      for (u32 h = 0; h < 2; ++h) {
+        const MxSixteen s = reinterpret_cast<const MxSixteen*>(p)[h];
+        w[i][h] = u32x4_t{s.w[0], s.w[1], s.w[2], s.w[3]};
+      }
+    } else {
+      w[i][0] = w[i][1] = u32x4_t{0, 0, 0, 0};
+      if (row < a.rows) {
 #pragma unroll
         for (u32 j = 0; j < N; ++j) {
           if (col + j >= a.cols) continue;
-          if constexpr (TYPE == ZC_F32) w[j / 4][j % 4] = __float_as_uint(p[j]);
-          else w[j / 8][j / 2 % 4] |= u32(__builtin_bit_cast(u16, p[j])) << (16 * (j & 1u));
+          if constexpr (TYPE == ZC_F32) w[i][j / 4][j % 4] = __float_as_uint(p[j]);
+          else w[i][j / 8][j / 2 % 4] |= u32(__builtin_bit_cast(u16, p[j])) << (16 * (j & 1u));
         }
       }
     }
-    if (DOWN) {
-      tile[in_tile * 16 + part * 2] = w[0];
-      tile[in_tile * 16 + part * 2 + 1] = w[1];
+  }
+  if (DOWN) {
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) {
+      tile[(32 * i + (tid >> 3)) * 16 + part * 2] = w[i][0];
+      tile[(32 * i + (tid >> 3)) * 16 + part * 2 + 1] = w[i][1];
     }
-    if (ALONG) {
-      u32 top = Pack::top_value(TYPE == ZC_F32 ? max(Pack::top(w[0]), Pack::top(w[1])) : max_pairs(Pack::top(w[0]), Pack::top(w[1])));
+  }
+  if (ALONG) {
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) {
+      const u64 row = row0 + 32 * i + (tid >> 3);
+      u32 top = Pack::top_value(TYPE == ZC_F32 ? max(Pack::top(w[i][0]), Pack::top(w[i][1])) : max_pairs(Pack::top(w[i][0]), Pack::top(w[i][1])));
       top = max(top, u32(__builtin_amdgcn_update_dpp(0, int(top), 0xB1, 0xf, 0xf, true)));                    // quad_perm 1 0 3 2
       if (LANES == 4) top = max(top, u32(__builtin_amdgcn_update_dpp(0, int(top), 0x4E, 0xf, 0xf, true)));    // quad_perm 2 3 0 1
       const u32 s = mx_scale(top);
       const float scale = divisor_value(s);
       const u64 block = col / kBlockValues;
-      if (row < a.rows && block * kBlockValues < a.cols) {
+      if (WHOLE || (row < a.rows && block * kBlockValues < a.cols)) {
         u8* const codes = a.held.codes + row * a.held.codes_stride + col / 2;
         if constexpr (TYPE == ZC_F32) {
-          const u32 eight[8] = {w[0][0], w[0][1], w[0][2], w[0][3], w[1][0], w[1][1], w[1][2], w[1][3]};
+          const u32 eight[8] = {w[i][0][0], w[i][0][1], w[i][0][2], w[i][0][3], w[i][1][0], w[i][1][1], w[i][1][2], w[i][1][3]};
           *reinterpret_cast<u32*>(codes) = codes_if(s, mx_codes<TYPE>(eight, scale));
         } else {
-          const u32 low[4] = {w[0][0], w[0][1], w[0][2], w[0][3]}, high[4] = {w[1][0], w[1][1], w[1][2], w[1][3]};
+          const u32 low[4] = {w[i][0][0], w[i][0][1], w[i][0][2], w[i][0][3]}, high[4] = {w[i][1][0], w[i][1][1], w[i][1][2], w[i][1][3]};
           *reinterpret_cast<u32x2_t*>(codes) = u32x2_t{codes_if(s, mx_codes<TYPE>(low, scale)), codes_if(s, mx_codes<TYPE>(high, scale))};
         }
         if (part % LANES == 0) a.held.scales[row * a.held.scales_stride + block] = u8(s);
@@ -163,7 +167,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 
   __syncthreads();
   const u32 lane = tid & 63u, wave = tid >> 6;
   const u64 block = row0 / kBlockValues + wave;
-  if (block * kBlockValues >= a.rows) return;
+  if (!WHOLE && block * kBlockValues >= a.rows) return;
   const u32* const words = reinterpret_cast<const u32*>(tile) + wave * (32 * kMxTileBytes / 4) + lane;
   u32 v[32];
   u32 top = 0;
@@ -175,7 +179,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 
 #pragma unroll
   for (u32 h = 0; h < (TYPE == ZC_F32 ? 1u : 2u); ++h) {
     const u64 c = col0 + (TYPE == ZC_F32 ? lane : 2 * lane + h);
-    if (c >= a.cols) break;
+    if (!WHOLE && c >= a.cols) break;
     const u32 s = mx_scale(TYPE == ZC_F32 ? top : Pack::top_value(h ? top >> 16 : top & 0xffffu));
     const float scale = divisor_value(s);
     u32x4_t codes;
@@ -183,19 +187,28 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 
     for (u32 q = 0; q < 4; ++q) {
       if constexpr (TYPE == ZC_F32) {
         const u32 eight[8] = {v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3], v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]};
-        codes[q] = mx_codes<TYPE>(eight, scale);
+        codes[q] = codes_if(s, mx_codes<TYPE>(eight, scale));
       } else {
         u32 four[4];                                    // two rows' values of the column side by side
 #pragma unroll
         for (u32 j = 0; j < 4; ++j) four[j] = __builtin_amdgcn_perm(v[8 * q + 2 * j + 1], v[8 * q + 2 * j], h ? 0x07060302u : 0x05040100u);
-        codes[q] = mx_codes<TYPE>(four, scale);
+        codes[q] = codes_if(s, mx_codes<TYPE>(four, scale));
       }
     }
-#pragma unroll
-    for (u32 q = 0; q < 4; ++q) codes[q] = codes_if(s, codes[q]);
     *reinterpret_cast<u32x4_t*>(a.held_t.codes + c * a.held_t.codes_stride + kMxBytes * block) = codes;
     a.held_t.scales[c * a.held_t.scales_stride + block] = u8(s);
   }
+}
+
+template <int TYPE, bool ALONG, bool DOWN>
+__global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 tiles_down, u32 tiles) {
+  constexpr u32 COLS = mx_tile_cols(TYPE);
+  __shared__ u32x4_t tile[DOWN ? kMxTileRows * kMxTileBytes / 16 : 1];
+  const u32 xcd = blockIdx.x & 7u, t = xcd * (tiles >> 3) + min(xcd, tiles & 7u) + (blockIdx.x >> 3);
+  const u32 across = t / tiles_down;
+  const u64 row0 = u64(t - across * tiles_down) * kMxTileRows, col0 = u64(across) * COLS;
+  if (row0 + kMxTileRows <= a.rows && col0 + COLS <= a.cols) mx_quantize_tile<TYPE, ALONG, DOWN, true>(a, row0, col0, tile);
+  else mx_quantize_tile<TYPE, ALONG, DOWN, false>(a, row0, col0, tile);
 }
 
 struct MxDequantizeArgs {
