@@ -1,6 +1,6 @@
 // One AdamW step over many tensors in one launch, with first and second moments in 32 bits or in 8.
 //
-// For every value (all steps in binary32, each rounded by itself; c.* come from binary64 on the host):
+// For every value (all steps in binary32, each rounded by itself, the root and the quotient within a unit in the last place; c.* come from binary64 on the host):
 //   g = grad x scale;  m' = b1 m + (1 - b1) g;  v' = b2 v + ((1 - b2) g) g;  r = sqrt(v')
 //   p' = p (1 - lr decay) - (lr / (1 - b1^t)) (m' / (r / sqrt(1 - b2^t) + eps))
 // In 8 bits a state holds m and r (the root: half the exponent range of v) as e4m3 codes, 32 values a block, the stream
@@ -66,12 +66,12 @@ __host__ __device__ inline u64 adamw_bytes(u64 blocks, int bits) {
   return bits == 32 ? 2 * adamw_second(blocks, 32) : adamw_scales(blocks) + 2 * pad16(blocks);
 }
 
-// Largest magnitude as bits (every NaN counts as more than infinity): of a lane's four values, and of 8 neighbouring lanes, in pairs, in fours
-// and with the mirrored half of the eight.
+// Largest magnitude of a lane's four values, and of 8 neighbouring lanes (in pairs, in fours and with the mirrored half of the eight), as bits without their sign,
+// shifted up by one: every NaN counts as more than infinity.
 __device__ inline u32 top_of_four(const float (&x)[4]) {
   u32 t = 0;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) t = max(t, __float_as_uint(x[j]) & 0x7fffffffu);
+  for (int j = 0; j < 4; ++j) t = max(t, __float_as_uint(x[j]) << 1);
   return t;
 }
 __device__ inline u32 top_of_eight(u32 x) {
@@ -82,16 +82,21 @@ __device__ inline u32 top_of_eight(u32 x) {
 
 // Scale byte of a block in 8 bits, from the largest magnitude.
 __device__ inline u32 adamw_scale(u32 top) {
-  const u32 e = top >> 23;
-  return e == 255u ? 255u : e > 7u ? e - 7u : 0u;
+  const u32 e = top >> 24;
+  return e == 255u ? 255u : max(e, 7u) - 7u;
 }
 
 // A magnitude scaled into the range of e4m3, on that format's grid: quanta of 2^-3 of the binade, of 2^-9 below 2^-6.
-__device__ inline float on_grid(float y, u32 random16, bool stochastic) {
+__device__ inline float nearest_on_grid(float y) {
   const u32 e = max(exponent_field(y), 121u);
-  const float t = y * power_of_two(257u - e);
-  const float k = stochastic ? floorf(t + float(random16) * 0x1p-16f) : rintf(t);
-  return k * power_of_two(e - 3u);
+  return rintf(y * power_of_two(257u - e)) * power_of_two(e - 3u);
+}
+// Up when the 16 random bits and the way from the grid's lower neighbour reach the upper one.  The grid's last place is bit 20 of a binary32; below 2^-6 it is so
+// once that much is added, which is taken off again.
+__device__ inline float random_on_grid(float y, u32 random16) {
+  const float lift = y < 0x1p-6f ? 0x1p-6f : 0.0f;
+  const u32 bits = __float_as_uint(y + lift) + (random16 << 4);
+  return __uint_as_float(bits & 0xfff00000u) - lift;
 }
 
 __device__ inline u32 four_codes(const float (&v)[4]) {
@@ -194,12 +199,11 @@ __device__ __forceinline__ void adamw_tile(const AdamwArgs& a, const AdamwEntry&
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       p[j] = float(raw_p[u].v[j]);
-      g[j] = float(raw_g[u].v[j]);
-      if (a.grad_scale) g[j] = g[j] * scale;
+      g[j] = float(raw_g[u].v[j]) * scale;
       m[j] = m[j] * c.b1 + g[j] * c.c1;
       v[j] = v[j] * c.b2 + (g[j] * c.c2) * g[j];
-      r[j] = sqrtf(v[j]);
-      p[j] = p[j] * c.keep - (m[j] / (r[j] * c.root + c.eps)) * c.rate;
+      r[j] = __builtin_amdgcn_sqrtf(v[j]);
+      p[j] = p[j] * c.keep - (m[j] * __builtin_amdgcn_rcpf(r[j] * c.root + c.eps)) * c.rate;
     }
     if (WHOLE || i + 4 <= x.n) {
       store_four<P>(x.param, i, p);
@@ -220,12 +224,21 @@ __device__ __forceinline__ void adamw_tile(const AdamwArgs& a, const AdamwEntry&
     } else {
       const u32 sm = adamw_scale(top_of_eight(top_of_four(m))), sr = adamw_scale(top_of_eight(top_of_four(r)));
       float cm[4], cr[4];
+      const float up_m = power_of_two(254u - min(sm, 253u)), up_r = power_of_two(254u - min(sr, 253u));
+      const u32 place = u32(s) * 0x9E3779B1u + a.key;
 #pragma unroll
       for (u32 j = 0; j < 4; ++j) {
-        const u32 z = mixed_word((u32(s) + j) * 0x9E3779B1u + a.key);
-        cm[j] = copysignf(on_grid(fabsf(m[j]) * power_of_two(254u - min(sm, 253u)), z & 0xffffu, a.stochastic), m[j]);
-        cr[j] = on_grid(r[j] * power_of_two(254u - min(sr, 253u)), z >> 16, a.stochastic);
-        if (r[j] > 0.0f) cr[j] = fmaxf(cr[j], 0x1p-9f);              // (a denominator never becomes none)
+        const float ym = fabsf(m[j]) * up_m, yr = r[j] * up_r;
+        if (a.stochastic) {
+          const u32 z = mixed_word(place + j * 0x9E3779B1u);
+          cm[j] = random_on_grid(ym, z & 0xffffu);
+          cr[j] = random_on_grid(yr, z >> 16);
+        } else {
+          cm[j] = nearest_on_grid(ym);
+          cr[j] = nearest_on_grid(yr);
+        }
+        cm[j] = copysignf(cm[j], m[j]);
+        cr[j] = fmaxf(cr[j], r[j] > 0.0f ? 0x1p-9f : 0.0f);          // (a denominator never becomes none)
       }
       if (WHOLE || i < padded) {
         u8* const scales = a.state + adamw_scales(a.blocks) + block;

@@ -119,9 +119,9 @@ template <int TYPE>
 int launch_quantize(const MxQuantizeArgs& a, hipStream_t stream) {
   const u64 down = (a.rows + kMxTileRows - 1) / kMxTileRows, across = (a.cols + mx_tile_cols(TYPE) - 1) / mx_tile_cols(TYPE), tiles = down * across;
   if (tiles > kMostGroups) return ZC_ERR_ARG;
-  if (a.held.codes && a.held_t.codes) hipLaunchKernelGGL((mx_quantize_kernel<TYPE, true, true>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(down), u32(tiles));
-  else if (a.held.codes) hipLaunchKernelGGL((mx_quantize_kernel<TYPE, true, false>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(down), u32(tiles));
-  else hipLaunchKernelGGL((mx_quantize_kernel<TYPE, false, true>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(down), u32(tiles));
+  if (a.held.codes && a.held_t.codes) hipLaunchKernelGGL((mx_quantize_kernel<TYPE, true, true>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(across));
+  else if (a.held.codes) hipLaunchKernelGGL((mx_quantize_kernel<TYPE, true, false>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(across));
+  else hipLaunchKernelGGL((mx_quantize_kernel<TYPE, false, true>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(across));
   return launched();
 }
 int quantize(const MxQuantizeArgs& a, hipStream_t stream) {

@@ -96,7 +96,8 @@ struct MxQuantizeArgs {
 // A workgroup takes 128 rows of 256 bytes (128 values of 16 bits, 64 of 32).  Eight threads a row hold 32 bytes each and make the blocks along the row
 // from their registers, two or four of them a block.  For the blocks down the columns the tile goes through LDS: wave w takes rows 32 w .. 32 w + 31, a
 // lane one column (of 32 bits) or two (of 16).  Memory sees every value once, whichever of the two are wanted.
-// Tiles follow each other down the matrix, so that what one XCD writes of a row of the transposed matrix lies together.
+// Tiles follow each other along the rows in the order of the workgroups: neighbours are read at the same time.  (Runs of tiles for each XCD, along the rows or down the columns, were slower
+// by 5 to 20 %: 8192 x 8192 in 16 bits along the rows 34 us, by runs 39; along both 50 and 52.)
 constexpr u32 kMxTileRows = 128, kMxTileBytes = 256;
 __host__ __device__ constexpr u32 mx_tile_cols(int type) { return kMxTileBytes / (type == ZC_F32 ? 4 : 2); }
 
@@ -201,12 +202,11 @@ __device__ __forceinline__ void mx_quantize_tile(const MxQuantizeArgs& a, u64 ro
 }
 
 template <int TYPE, bool ALONG, bool DOWN>
-__global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 tiles_down, u32 tiles) {
+__global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 tiles_across) {
   constexpr u32 COLS = mx_tile_cols(TYPE);
   __shared__ u32x4_t tile[DOWN ? kMxTileRows * kMxTileBytes / 16 : 1];
-  const u32 xcd = blockIdx.x & 7u, t = xcd * (tiles >> 3) + min(xcd, tiles & 7u) + (blockIdx.x >> 3);
-  const u32 across = t / tiles_down;
-  const u64 row0 = u64(t - across * tiles_down) * kMxTileRows, col0 = u64(across) * COLS;
+  const u32 down = blockIdx.x / tiles_across;
+  const u64 row0 = u64(down) * kMxTileRows, col0 = u64(blockIdx.x - down * tiles_across) * COLS;
   if (row0 + kMxTileRows <= a.rows && col0 + COLS <= a.cols) mx_quantize_tile<TYPE, ALONG, DOWN, true>(a, row0, col0, tile);
   else mx_quantize_tile<TYPE, ALONG, DOWN, false>(a, row0, col0, tile);
 }
