@@ -264,31 +264,33 @@ __global__ __launch_bounds__(256, TM * TN > 4 ? 1 : 2) void mx_tile_kernel(MxPro
     rows_b.move_on(128);
   };
   u32x4_t held[SCALE_LOADS];
-  const auto ask_scales = [&] {                         // 16 scale bytes of a row for the pair that is asked for, 16 for the next one; those behind the last block as zeros
+  const auto of_a = [&](u32 i) { return RA % 128 == 0 ? 128 * i < RA : 32 * wave + 128 * i < RA; };     // whose rows the loads are of
+  u32 scales_at[SCALE_LOADS];
 #pragma unroll
-    for (u32 i = 0; i < SCALE_LOADS; ++i) {
-      const u32 row = (tid >> 1) + 128 * i;
-      const bool of_a = 32 * wave + 128 * i < RA;
-      const u32 at = (of_a ? row * u32(a.a_scales_stride) : (row - RA) * u32(a.b_scales_stride)) + 16 * (tid & 1u);
-      const __amdgpu_buffer_rsrc_t from = of_a ? scales_a.buffer() : scales_b.buffer();
-      if (16 * ask_pair + 32 <= a.blocks) {
-        held[i] = __builtin_amdgcn_raw_buffer_load_b128(from, at, 0, 0);
-      } else {
+  for (u32 i = 0; i < SCALE_LOADS; ++i) {
+    const u32 row = (tid >> 1) + 128 * i;
+    scales_at[i] = (of_a(i) ? row * u32(a.a_scales_stride) : (row - RA) * u32(a.b_scales_stride)) + 16 * (tid & 1u);
+  }
+  const auto ask_scales = [&] {                         // 16 scale bytes of a row for the pair that is asked for, 16 for the next one; those behind the last block as zeros
+    if (16 * ask_pair + 32 <= a.blocks) {
+#pragma unroll
+      for (u32 i = 0; i < SCALE_LOADS; ++i) held[i] = __builtin_amdgcn_raw_buffer_load_b128(of_a(i) ? scales_a.buffer() : scales_b.buffer(), scales_at[i], 0, 0);
+    } else {
+#pragma unroll
+      for (u32 i = 0; i < SCALE_LOADS; ++i)
 #pragma unroll
         for (u32 j = 0; j < 4; ++j) {
           const u32 first = 16 * (ask_pair + (tid & 1u)) + 4 * j;
-          const u32 w = __builtin_amdgcn_raw_buffer_load_b32(from, first < a.blocks ? at + 4 * j : ~0u, 0, 0);
+          const u32 w = __builtin_amdgcn_raw_buffer_load_b32(of_a(i) ? scales_a.buffer() : scales_b.buffer(), first < a.blocks ? scales_at[i] + 4 * j : ~0u, 0, 0);
           held[i][j] = first + 4 <= a.blocks || first >= a.blocks ? w : w & ((1u << (8 * (a.blocks - first))) - 1u);
         }
-      }
     }
   };
   const auto put_scales = [&](u32 plane) {              // into this plane and the next one
 #pragma unroll
     for (u32 i = 0; i < SCALE_LOADS; ++i) {
       const u32 row = (tid >> 1) + 128 * i;
-      const bool of_a = 32 * wave + 128 * i < RA;
-      memory[(of_a ? AT_SCALES_A : AT_SCALES_B - RA * 16) / 16 + (plane + (tid & 1u)) * (of_a ? RA : RB) + row] = held[i];
+      memory[(of_a(i) ? AT_SCALES_A : AT_SCALES_B - RA * 16) / 16 + (plane + (tid & 1u)) * (of_a(i) ? RA : RB) + row] = held[i];
     }
   };
 
