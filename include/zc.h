@@ -341,7 +341,7 @@ int zc_adamw(int k, const size_t* n, void* const* d_params, int param_type, cons
  * 2^(s - 127), 255 for a block with a value that is not finite (32 NaNs, codes 0).  s is the exponent field of the block's largest magnitude
  * minus 2, at least 0; codes are rounded to the nearest, ties to even, and at most 6.  The last block of a row is filled up with zeros.
  * Codes: rows codes_stride bytes apart, a multiple of 16, 16-byte aligned.  Scale bytes: rows scales_stride bytes
- * apart, a multiple of 4, 4-byte aligned.  The smallest strides: */
+ * apart, a multiple of 4, 4-byte aligned (they are read by whole words of 4).  The smallest strides: */
 size_t zc_mx_codes_stride(size_t cols);
 size_t zc_mx_scales_stride(size_t cols);
 

@@ -93,13 +93,17 @@ void launch_tiles(const MxProductArgs& a, hipStream_t stream) {
 
 int product(const MxProductArgs& a, hipStream_t stream) {
   if (a.m == 0 || a.n == 0) return ZC_OK;
+  if (((a.m + 63) / 64) * ((a.n + 63) / 64) > kMostGroups) return ZC_ERR_ARG;
   if (a.m <= kFewRows) return launch_few<kHeldRows>(MxFewArgs{a, nullptr, 0, 0, 0}, stream);
   if (a.blocks > 0 && a.a_stride <= kMostTileStride && a.b_stride <= kMostTileStride && a.a_scales_stride <= kMostTileStride && a.b_scales_stride <= kMostTileStride) {
-    const u64 t4 = ((a.m + 255) / 256) * ((a.n + 255) / 256), t2 = ((a.m + 127) / 128) * ((a.n + 127) / 128), t1 = ((a.m + 63) / 64) * ((a.n + 63) / 64);
-    if (t4 >= 200) launch_tiles<4>(a, stream);
-    else if (t2 >= 200) launch_tiles<2>(a, stream);
+    // The size of tile that takes the least time, in us, by what a turn of all CUs has been measured to take: a tile's begin and end, and 4096 values along k.
+    // (4096 x 4096 x 4096 by tiles of 256, 128 and 64: 39, 43 and 63 us; 1024 x 4096 x 4096: 26, 14 and 19; 333 x 1531 x 1000: 18, 7.4 and 4.6.)
+    const double along = double(a.blocks) / 128;
+    const auto turns = [&](u64 rows) { return double(((a.m + rows - 1) / rows * ((a.n + rows - 1) / rows) + 255) / 256); };
+    const double large = turns(256) * (14.8 + 25.0 * along), middle = 3.0 + turns(128) * (2.6 + 8.9 * along), small = 3.0 + turns(64) * (0.6 + 3.4 * along);
+    if (large <= middle && large <= small) launch_tiles<4>(a, stream);
+    else if (middle <= small) launch_tiles<2>(a, stream);
     else launch_tiles<1>(a, stream);
-    (void)t1;
     return launched();
   }
   const u64 down = (a.m + 15) / 16, across = (a.n + 15) / 16;
