@@ -1,6 +1,7 @@
 // One AdamW step over many tensors in one launch, with first and second moments in 32 bits or in 8.
 //
-// For every value (all steps in binary32, each rounded by itself, the root and the quotient within a unit in the last place; c.* come from binary64 on the host):
+// For every value (all steps in binary32, each rounded by itself, except that the quotient, and the root where it is not stored, are within
+// a unit in the last place; c.* come from binary64 on the host):
 //   g = grad x scale;  m' = b1 m + (1 - b1) g;  v' = b2 v + ((1 - b2) g) g;  r = sqrt(v')
 //   p' = p (1 - lr decay) - (lr / (1 - b1^t)) (m' / (r / sqrt(1 - b2^t) + eps))
 // In 8 bits a state holds m and r (the root: half the exponent range of v) as e4m3 codes, 32 values a block, the stream
@@ -91,12 +92,12 @@ __device__ inline float nearest_on_grid(float y) {
   const u32 e = max(exponent_field(y), 121u);
   return rintf(y * power_of_two(257u - e)) * power_of_two(e - 3u);
 }
-// Up when the 16 random bits and the way from the grid's lower neighbour reach the upper one.  The grid's last place is bit 20 of a binary32; below 2^-6 it is so
-// once that much is added, which is taken off again.
+// Up when the 16 random bits and the way from the grid's lower neighbour reach the upper one: floor(y / quantum + random / 65536) quanta.  The last place that stays of a
+// binary32 is its bit 20, so that is a sum of integers, except below 2^-6, where the quanta no longer shrink.
 __device__ inline float random_on_grid(float y, u32 random16) {
-  const float lift = y < 0x1p-6f ? 0x1p-6f : 0.0f;
-  const u32 bits = __float_as_uint(y + lift) + (random16 << 4);
-  return __uint_as_float(bits & 0xfff00000u) - lift;
+  const u32 bits = __float_as_uint(y) + (random16 << 4);
+  const float low = floorf(__builtin_fmaf(float(random16), 0x1p-16f, y * 0x1p9f)) * 0x1p-9f;
+  return y < 0x1p-6f ? low : __uint_as_float(bits & 0xfff00000u);
 }
 
 __device__ inline u32 four_codes(const float (&v)[4]) {
@@ -202,7 +203,7 @@ __device__ __forceinline__ void adamw_tile(const AdamwArgs& a, const AdamwEntry&
       g[j] = float(raw_g[u].v[j]) * scale;
       m[j] = m[j] * c.b1 + g[j] * c.c1;
       v[j] = v[j] * c.b2 + (g[j] * c.c2) * g[j];
-      r[j] = __builtin_amdgcn_sqrtf(v[j]);
+      r[j] = BITS == 8 ? sqrtf(v[j]) : __builtin_amdgcn_sqrtf(v[j]);
       p[j] = p[j] * c.keep - (m[j] * __builtin_amdgcn_rcpf(r[j] * c.root + c.eps)) * c.rate;
     }
     if (WHOLE || i + 4 <= x.n) {
