@@ -196,7 +196,8 @@ int zc_adamw(int k, const size_t* n, void* const* d_params, int param_type, cons
       block += num_blocks(now);
     }
   }
-  if (a.tensors) go();
+  if (!a.tensors) return ZC_OK;                                      // (no values at all)
+  go();
   return launched();
 }
 
