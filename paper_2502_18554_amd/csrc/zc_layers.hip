@@ -16,7 +16,9 @@ namespace {
 bool aligned(const void* p, u64 to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 bool type_valid(int type) { return type == ZC_F32 || type == ZC_BF16 || type == ZC_F16; }
 int launched() { return hipGetLastError() == hipSuccess ? ZC_OK : ZC_ERR_HIP; }
-constexpr u64 kMostGroups = 0x7fffffffu;
+constexpr u64 kMostGroups = 0xffffffu;             // of 256 threads: a grid has less than 2^32 threads
+constexpr u64 kMostTiles = 0x7fffffffu;            // that a persistent grid counts
+constexpr u64 kMostCols = u64(1) << 28;            // of a product's one launch, with the same limit
 
 template <int P, int G>
 void launch_adamw(const AdamwArgs& a, u32 tiles, int bits, hipStream_t stream) {
@@ -79,11 +81,6 @@ int launch_few(const MxFewArgs& a, hipStream_t stream) {
   if (a.p.n >= 2 * 16 * 256) return launch_few<RG, 2, X>(a, stream);
   return launch_few<RG, 1, X>(a, stream);
 }
-template <int X>
-int launch_few(const MxFewArgs& a, hipStream_t stream) {
-  return a.p.m <= 16 ? launch_few<1, X>(a, stream) : launch_few<2, X>(a, stream);
-}
-
 template <int T>
 void launch_tiles(const MxProductArgs& a, hipStream_t stream) {
   if (a.out_type == ZC_F32) launch_tiles<T, ZC_F32>(a, stream);
@@ -91,10 +88,27 @@ void launch_tiles(const MxProductArgs& a, hipStream_t stream) {
   else launch_tiles<T, ZC_F16>(a, stream);
 }
 
-int product(const MxProductArgs& a, hipStream_t stream) {
-  if (a.m == 0 || a.n == 0) return ZC_OK;
-  if (((a.m + 63) / 64) * ((a.n + 63) / 64) > kMostGroups) return ZC_ERR_ARG;
-  if (a.m <= kFewRows) return launch_few<kHeldRows>(MxFewArgs{a, nullptr, 0, 0, 0}, stream);
+// Calls `launch` for the columns of a product, kMostCols at a time.
+template <typename F>
+int by_columns(const MxProductArgs& a, const F& launch) {
+  for (u64 at = 0; at < a.n; at += kMostCols) {
+    MxProductArgs part = a;
+    part.n = a.n - at < kMostCols ? a.n - at : kMostCols;
+    part.b += at * a.b_stride;
+    part.b_scales += at * a.b_scales_stride;
+    if (a.bias) part.bias += at;
+    part.out = static_cast<u8*>(a.out) + at * value_bytes(a.out_type);
+    const int st = launch(part);
+    if (st != ZC_OK) return st;
+  }
+  return ZC_OK;
+}
+
+int product_launch(const MxProductArgs& a, hipStream_t stream) {
+  if (a.m <= kFewRows) {
+    const MxFewArgs few{a, nullptr, 0, 0, 0};
+    return a.m <= 16 ? launch_few<1, kHeldRows>(few, stream) : launch_few<2, kHeldRows>(few, stream);
+  }
   if (a.blocks > 0 && a.a_stride <= kMostTileStride && a.b_stride <= kMostTileStride && a.a_scales_stride <= kMostTileStride && a.b_scales_stride <= kMostTileStride) {
     // The size of tile that takes the least time, in us, by what a turn of all CUs has been measured to take: a tile's begin and end, and 4096 values along k.
     // (4096 x 4096 x 4096 by tiles of 256, 128 and 64: 39, 43 and 63 us; 1024 x 4096 x 4096: 26, 14 and 19; 333 x 1531 x 1000: 18, 7.4 and 4.6.)
@@ -117,6 +131,11 @@ int product(const MxProductArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(mx_product_kernel, dim3(u32(across), u32(left < 65535 ? left : 65535)), dim3(64), 0, stream, part);
   }
   return launched();
+}
+int product(const MxProductArgs& a, hipStream_t stream) {
+  if (a.m == 0 || a.n == 0) return ZC_OK;
+  if (((a.m + 63) / 64) * ((a.n + 63) / 64) > kMostTiles) return ZC_ERR_ARG;
+  return by_columns(a, [&](const MxProductArgs& part) { return product_launch(part, stream); });
 }
 
 template <int TYPE>
@@ -291,9 +310,14 @@ int zc_mx_linear(const void* d_x, int x_type, size_t x_stride, const void* d_w, 
   a.out_type = out_type;
   a.add = flags & ZC_MX_ADD;
   hipStream_t const stream = static_cast<hipStream_t>(hip_stream);
-  if (m <= kFewRows && x_stride <= kMostFewStride) {
-    const MxFewArgs few{a, d_x, x_stride, k, 0};
-    return x_type == ZC_F32 ? launch_few<ZC_F32>(few, stream) : x_type == ZC_BF16 ? launch_few<ZC_BF16>(few, stream) : launch_few<ZC_F16>(few, stream);
+  // Up to 8 rows are quantised by the product's own waves, each of which does so again for its 16 CG columns; more rows take longer so than a launch of their own.
+  // (In this kernel against both, GPU time: 4096 x 4096 by 1, 8 and 16 rows 4.3, 5.6 and 6.8 us against 5.4, 5.9 and 6.3; 16384 x 4096 by 1, 8, 16 and 32 rows
+  // 9.9, 10.5, 11.6 and 16.8 against 10.3, 10.5, 10.9 and 13.1.  8 rows by two launches cost the caller's thread another 2.5 us besides.)
+  if (m <= kFewValueRows && x_stride <= kMostFewStride) {
+    return by_columns(a, [&](const MxProductArgs& part) {
+      const MxFewArgs few{part, d_x, x_stride, k, 0};
+      return x_type == ZC_F32 ? launch_few<1, ZC_F32>(few, stream) : x_type == ZC_BF16 ? launch_few<1, ZC_BF16>(few, stream) : launch_few<1, ZC_F16>(few, stream);
+    });
   }
   const int st = zc_mx_quantize(d_x, x_type, m, k, x_stride, codes, codes_stride, scales, scales_stride, nullptr, 0, nullptr, 0, hip_stream);
   return st != ZC_OK ? st : product(a, stream);

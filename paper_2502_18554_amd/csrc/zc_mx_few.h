@@ -2,16 +2,16 @@
 //
 // A workgroup makes all rows' results of 16 CG columns; its waves take turns along k, by spans of 16 blocks, and add up in LDS in the end, wave by wave, so that
 // a sum's order depends on the sizes only.  A wave reads four blocks (64 bytes) of 16 rows of b with one load, and keeps the loads of a span in flight.
-// Rows of a come as they are held, or as values: then a lane quantises the block that it brings to the instruction, in registers: some 60 operations for every four
-// loads, hidden behind them, where a launch of its own for that takes longer than the product.
+// Rows of a come as they are held, or (up to 8) as values: then a lane quantises the block that it brings to the instruction, in registers: some 60 operations for
+// every four loads, mostly hidden behind them, where a launch of its own for that takes half as long as the product.
 #pragma once
 
 #include "zc_mx_product.h"
 
 namespace zc {
 
-constexpr u64 kMostFewStride = u64(1) << 24;     // (32 rows of values are less than 2^32 bytes)
-constexpr u32 kFewRows = 32, kFewWaves = 8, kSpanOfBlocks = 16;
+constexpr u64 kMostFewStride = u64(1) << 24;     // (8 rows of values are less than 2^32 bytes)
+constexpr u32 kFewRows = 32, kFewValueRows = 8, kFewWaves = 8, kSpanOfBlocks = 16;
 constexpr int kHeldRows = -1;                    // the type of rows that are held in 4 bits
 
 struct MxFewArgs {
