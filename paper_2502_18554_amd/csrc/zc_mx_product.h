@@ -127,6 +127,14 @@ __device__ inline void swap_halves(u32& a, u32& b) {
   a = r[0], b = r[1];
 }
 
+// The compiler has to have these sums here, in the matrix instructions' own registers where a wave has more of them than the others would hold (of those
+// every value has to be moved before it can be written: 2048 x 2048 x 2048 10.0 us, 10.3 so).
+template <int OF>
+__device__ __forceinline__ void mx_hold(f32x16_t& sum) {
+  if constexpr (OF > 4) asm volatile("" : "+a"(sum));
+  else asm volatile("" : "+v"(sum));
+}
+
 // Two neighbouring values of a type, rounded, as a word; a value of 32 bits is one.
 template <int TYPE>
 __device__ inline u32 packed_pair(float low, float high) {
@@ -137,48 +145,40 @@ __device__ inline u32 packed_pair(float low, float high) {
 
 // The results of a wave: row0 and col0 are its tile's first.  Lane l has, of 32 x 32, 16 neighbouring ones of row l % 32, from column 16 (l / 32) on.  Its pieces of 16 bytes go to
 // other lanes so that four lanes write 64 bytes of a row together (16 rows a store): single pieces would be that many more requests to L2.
-// WHOLE: the matrix has all of these results.
-template <int TM, int TN, int TYPE, bool WHOLE>
+// WHOLE: the matrix has all of these results.  MORE: there may be a bias, or something to add to; then the sums themselves change lanes, and what is added is
+// read as the results are written, 16 bytes a lane (333 x 1531 x 1000 with both 6.4 us; a value at a time, where a lane's sums were, 9.3).
+template <int TM, int TN, int TYPE, bool WHOLE, bool MORE>
 __device__ __forceinline__ void mx_write_tile(const MxProductArgs& a, u64 row0, u64 col0, u32 lane, f32x16_t (&sum)[TM][TN]) {
   using One = typename ValueOf<TYPE>::One;
   constexpr u32 N = 16 / sizeof(One), PIECES = 16 / N;   // values of a piece; a lane's pieces
   struct __attribute__((packed, aligned(2))) Piece { u32 w[4]; };
-  const u64 own_row0 = row0 + (lane & 31u), own_col0 = col0 + 16 * (lane >> 5);
   const u64 to_row0 = row0 + (lane & 15u), to_col0 = col0 + N * (lane >> 4);
   One* const to0 = static_cast<One*>(a.out) + to_row0 * a.out_stride + to_col0;
+  // How many rows and columns there are from a lane's first on: what exceeds a tile does not matter.
+  const int rows_left = int(min(i64(a.m) - i64(to_row0), i64(1024))), cols_left = int(max(min(i64(a.n) - i64(to_col0), i64(1024)), i64(-1024)));
 #pragma unroll
   for (int j = 0; j < TN; ++j) {
-    const u64 own_col = own_col0 + 32 * j;
-    float bias[16];
-    if (a.bias) {
+    float bias[8] = {};                                  // (added where there is none as well: loads that a branch may leave unused would be waited for in the next tile)
+    if (MORE && a.bias) {
 #pragma unroll
-      for (u32 c = 0; c < 16; ++c) bias[c] = WHOLE || own_col + c < a.n ? a.bias[own_col + c] : 0.0f;
+      for (u32 c = 0; c < 8; ++c) {
+        const u64 col = to_col0 + 32 * j + (TYPE == ZC_F32 ? 16 * (c / 4) + c % 4 : c);
+        bias[c] = a.bias[WHOLE ? col : min(col, a.n - 1)];                       // (of columns that there are none of: any)
+      }
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      asm volatile("" : "+a"(sum[i][j]));                // (leaves the results in their registers until they are wanted)
-      float v[16];
+      mx_hold<TM * TN>(sum[i][j]);                       // (leaves the results in their registers until they are wanted)
+      // The words that change lanes: rounded values in pairs, or, where something is added first, the sums.
+      constexpr u32 WORDS = MORE || TYPE == ZC_F32 ? N : 4;
+      u32 w[PIECES][WORDS];
 #pragma unroll
-      for (u32 c = 0; c < 16; ++c) v[c] = sum[i][j][c];
-      if (a.bias) {
-#pragma unroll
-        for (u32 c = 0; c < 16; ++c) v[c] += bias[c];
-      }
-      const u64 own_row = own_row0 + 32 * i;
-      if (a.add && (WHOLE || own_row < a.m)) {
-        const One* const before = static_cast<const One*>(a.out) + own_row * a.out_stride + own_col;
-#pragma unroll
-        for (u32 c = 0; c < 16; ++c)
-          if (WHOLE || own_col + c < a.n) v[c] += float(before[c]);
-      }
-      u32 w[PIECES][4];
-#pragma unroll
-      for (u32 d = 0; d < 4 * PIECES; ++d) {
-        if constexpr (TYPE == ZC_F32) w[d / 4][d % 4] = __float_as_uint(v[d]);
-        else w[d / 4][d % 4] = packed_pair<TYPE>(v[2 * d], v[2 * d + 1]);
+      for (u32 d = 0; d < WORDS * PIECES; ++d) {
+        if constexpr (WORDS == N) w[d / N][d % N] = __float_as_uint(sum[i][j][d]);
+        else w[d / 4][d % 4] = packed_pair<TYPE>(sum[i][j][2 * d], sum[i][j][2 * d + 1]);
       }
 #pragma unroll
-      for (u32 d = 0; d < 4; ++d) {
+      for (u32 d = 0; d < WORDS; ++d) {
         if constexpr (PIECES == 4) {
           swap_halves(w[0][d], w[2][d]);
           swap_halves(w[1][d], w[3][d]);
@@ -190,16 +190,50 @@ __device__ __forceinline__ void mx_write_tile(const MxProductArgs& a, u64 row0, 
 #pragma unroll
       for (u32 q = 0; q < PIECES; ++q) {
         One* const to = to0 + (32 * i + 16 * (q & 1u)) * a.out_stride + (32 * j + 4 * N * (q / 2));
-        const u64 row = to_row0 + 32 * i + 16 * (q & 1u), col = to_col0 + 32 * j + 4 * N * (q / 2);
-        if (WHOLE || (row < a.m && col + N <= a.n)) {
-          *reinterpret_cast<Piece*>(to) = Piece{{w[q][0], w[q][1], w[q][2], w[q][3]}};
-        } else if (row < a.m && col < a.n) {
-          asm volatile("" ::: "memory");                 // (keeps the stores above in one piece)
-          One piece[N];
-          __builtin_memcpy(piece, w[q], 16);
+        const int left = WHOLE || rows_left > int(32 * i + 16 * (q & 1u)) ? cols_left - int(32 * j + 4 * N * (q / 2)) : 0;
+        Piece piece;
+        if constexpr (MORE) {
+          float v[N];
 #pragma unroll
-          for (u32 c = 0; c < N; ++c)
-            if (col + c < a.n) to[c] = piece[c];
+          for (u32 c = 0; c < N; ++c) v[c] = __uint_as_float(w[q][c]);
+#pragma unroll
+          for (u32 c = 0; c < N; ++c) v[c] += bias[TYPE == ZC_F32 ? 4 * (q / 2) + c : c];
+          if (a.add) {
+            One before[N] = {};
+            if (WHOLE || left >= int(N)) {
+              piece = *reinterpret_cast<const Piece*>(to);
+              __builtin_memcpy(before, &piece, 16);
+            } else if (left > 0) {
+#pragma unroll
+              for (u32 c = 0; c < N; ++c) before[c] = to[min(int(c), left - 1)];
+            }
+#pragma unroll
+            for (u32 c = 0; c < N; ++c) v[c] += float(before[c]);
+          }
+#pragma unroll
+          for (u32 d = 0; d < 4; ++d) {
+            if constexpr (TYPE == ZC_F32) piece.w[d] = __float_as_uint(v[d]);
+            else piece.w[d] = packed_pair<TYPE>(v[2 * d], v[2 * d + 1]);
+          }
+        } else {
+          piece = Piece{{w[q][0], w[q][1], w[q][2], w[q][3]}};
+        }
+        if (WHOLE || left >= int(N)) {
+          *reinterpret_cast<Piece*>(to) = piece;
+        } else if (left > 0) {
+          u32 d[4] = {piece.w[0], piece.w[1], piece.w[2], piece.w[3]};
+#pragma unroll 1
+          for (int c = 0; c < left; ++c) {               // one by one from the low end, as the rest moves down
+            asm volatile("" ::: "memory");               // (keeps the stores above in one piece)
+            if constexpr (TYPE == ZC_F32) {
+              to[c] = __uint_as_float(d[0]);
+              d[0] = d[1], d[1] = d[2], d[2] = d[3];
+            } else {
+              to[c] = __builtin_bit_cast(One, u16(d[0]));
+#pragma unroll
+              for (u32 e = 0; e < 4; ++e) d[e] = d[e] >> 16 | (e < 3 ? d[e + 1] << 16 : 0u);
+            }
+          }
         }
       }
     }
@@ -207,7 +241,7 @@ __device__ __forceinline__ void mx_write_tile(const MxProductArgs& a, u64 row0, 
 }
 
 template <int TM, int TN, int TYPE>
-__global__ __launch_bounds__(256, TM * TN > 4 ? 1 : 2) void mx_tile_kernel(MxProductArgs a, u32 tiles_down, u32 tiles_across) {
+__global__ __launch_bounds__(256, TM * TN > 4 ? 1 : TM * TN > 1 ? 2 : 4) void mx_tile_kernel(MxProductArgs a, u32 tiles_down, u32 tiles_across) {
   constexpr u32 RA = mx_tile_rows(TM), RB = mx_tile_rows(TN), ROWS = RA + RB, LOADS = ROWS / 32;
   constexpr u32 SCALE_LOADS = ROWS / 128;
   // In LDS: two stages of a's rows, two of b's, the scale bytes of four pairs of stages of a's rows, of b's.
@@ -371,7 +405,7 @@ __global__ __launch_bounds__(256, TM * TN > 4 ? 1 : 2) void mx_tile_kernel(MxPro
             if (t == 1) sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, x, sum[i][j], kMxFp4, kMxFp4, 1, scale_b, 1, scale_a);
             if (t == 2) sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, x, sum[i][j], kMxFp4, kMxFp4, 2, scale_b, 2, scale_a);
             if (t == 3) sum[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, x, sum[i][j], kMxFp4, kMxFp4, 3, scale_b, 3, scale_a);
-            asm volatile("" : "+a"(sum[i][j]));          // (holds the instruction at its place)
+            mx_hold<TM * TN>(sum[i][j]);                 // (holds the instruction at its place)
             __builtin_amdgcn_sched_barrier(0);
           }
           if (t == 0) next_stage();
@@ -386,8 +420,11 @@ __global__ __launch_bounds__(256, TM * TN > 4 ? 1 : 2) void mx_tile_kernel(MxPro
     u32 down, across;
     tiles.place(tile, down, across);
     const u64 row0 = u64(down) * RA + wave_a, col0 = u64(across) * RB + wave_b;
-    if (row0 + 32 * TM <= a.m && col0 + 32 * TN <= a.n) mx_write_tile<TM, TN, TYPE, true>(a, row0, col0, lane, sum);
-    else mx_write_tile<TM, TN, TYPE, false>(a, row0, col0, lane, sum);
+    const bool whole = row0 + 32 * TM <= a.m && col0 + 32 * TN <= a.n, more = a.bias || a.add;
+    if (whole && !more) mx_write_tile<TM, TN, TYPE, true, false>(a, row0, col0, lane, sum);
+    else if (whole) mx_write_tile<TM, TN, TYPE, true, true>(a, row0, col0, lane, sum);
+    else if (!more) mx_write_tile<TM, TN, TYPE, false, false>(a, row0, col0, lane, sum);
+    else mx_write_tile<TM, TN, TYPE, false, true>(a, row0, col0, lane, sum);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (the last requests, too, before the workgroup's LDS is given to another one)
 }
