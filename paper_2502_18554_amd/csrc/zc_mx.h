@@ -103,11 +103,47 @@ __host__ __device__ constexpr u32 mx_tile_cols(int type) { return kMxTileBytes /
 
 struct __attribute__((packed, aligned(2))) MxSixteen { u32 w[4]; };
 
-// WHOLE: the matrix has all of the tile; then nothing is asked about between the loads, and all of them are on their way together.
-template <int TYPE, bool ALONG, bool DOWN, bool WHOLE>
+// What a tile's loads have to look after: nothing, as the matrix has all of it; the matrix's end; rows of less than 16 bytes.
+enum MxEdge { kWholeTile, kEdgeTile, kNarrowTile };
+
+// 16 bytes of a row from a column on.  Those that the row's end cuts off are the row's last 16, which mx_cut then moves down: loads of single values took up to twice as
+// long (333 x 1000 in 16 bits along the rows 2.9 us, 6.1 so).
+template <int TYPE, MxEdge EDGE>
+__device__ __forceinline__ u32x4_t mx_load_sixteen(const typename ValueOf<TYPE>::One* row, u64 col, u64 cols) {
+  constexpr u32 K = MxPack<TYPE>::kValues;
+  if constexpr (EDGE != kNarrowTile) {
+    const MxSixteen s = *reinterpret_cast<const MxSixteen*>(row + (EDGE == kWholeTile ? col : min(col, cols - K)));
+    return u32x4_t{s.w[0], s.w[1], s.w[2], s.w[3]};
+  } else {
+    u32x4_t w = {0, 0, 0, 0};
+#pragma unroll
+    for (u32 j = 0; j < K; ++j) {
+      const auto one = row[min(u64(j), cols - 1)];
+      const bool there = col == 0 && j < cols;
+      if constexpr (TYPE == ZC_F32) w[j] = there ? __float_as_uint(one) : 0u;
+      else w[j / 2] |= (there ? u32(__builtin_bit_cast(u16, one)) : 0u) << (16 * (j & 1u));
+    }
+    return w;
+  }
+}
+template <int TYPE>
+__device__ __forceinline__ u32x4_t mx_cut(u32x4_t w, int left) {                            // (left: the row's values from the column on)
+  constexpr int K = MxPack<TYPE>::kValues;
+  const u32 by = u32(K - max(min(left, K), 0));          // values to move
+  const u32 words = TYPE == ZC_F32 ? by : by / 2;
+  if (TYPE != ZC_F32 && by % 2) w = u32x4_t{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
+  if (words & 1u) w = u32x4_t{w[1], w[2], w[3], 0};
+  if (words & 2u) w = u32x4_t{w[2], w[3], 0, 0};
+  if (words & 4u) w = u32x4_t{0, 0, 0, 0};
+  return w;
+}
+
+// (Nothing is asked about between the loads, so that all of them are on their way together.)
+template <int TYPE, bool ALONG, bool DOWN, MxEdge EDGE>
 __device__ __forceinline__ void mx_quantize_tile(const MxQuantizeArgs& a, u64 row0, u64 col0, u32x4_t* tile) {
   using One = typename ValueOf<TYPE>::One;
   using Pack = MxPack<TYPE>;
+  constexpr bool WHOLE = EDGE == kWholeTile;
   constexpr u32 N = 2 * Pack::kValues, LANES = kBlockValues / N;          // values of a thread, of a row; threads of a block
   const u32 tid = threadIdx.x, part = tid & 7u;
   const u64 col = col0 + part * N;
@@ -115,24 +151,24 @@ __device__ __forceinline__ void mx_quantize_tile(const MxQuantizeArgs& a, u64 ro
 #pragma unroll
   for (u32 i = 0; i < 4; ++i) {
     const u64 row = row0 + 32 * i + (tid >> 3);
-    const One* const p = static_cast<const One*>(a.in) + row * a.stride + col;
-    if (WHOLE || (row < a.rows && col + N <= a.cols)) {
+    const One* const p = static_cast<const One*>(a.in) + (WHOLE ? row : min(row, a.rows - 1)) * a.stride;
+#pragma unroll
+    for (u32 h = 0; h < 2; ++h) w[i][h] = mx_load_sixteen<TYPE, EDGE>(p, col + Pack::kValues * h, a.cols);
+  }
+  if (!WHOLE) {
+    const int left = int(max(min(i64(a.cols) - i64(col), i64(1024)), i64(0)));
+    if (EDGE == kEdgeTile && col0 + 8 * N > a.cols) {
+#pragma unroll
+      for (u32 i = 0; i < 4; ++i)
+#pragma unroll
+        for (u32 h = 0; h < 2; ++h) w[i][h] = mx_cut<TYPE>(w[i][h], left - int(Pack::kValues * h));
+    }
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i)
 #pragma unroll
       for (u32 h = 0; h < 2; ++h) {
-        const MxSixteen s = reinterpret_cast<const MxSixteen*>(p)[h];
-        w[i][h] = u32x4_t{s.w[0], s.w[1], s.w[2], s.w[3]};
+        if (row0 + 32 * i + (tid >> 3) >= a.rows) w[i][h] = u32x4_t{0, 0, 0, 0};
       }
-    } else {
-      w[i][0] = w[i][1] = u32x4_t{0, 0, 0, 0};
-      if (row < a.rows) {
-#pragma unroll
-        for (u32 j = 0; j < N; ++j) {
-          if (col + j >= a.cols) continue;
-          if constexpr (TYPE == ZC_F32) w[i][j / 4][j % 4] = __float_as_uint(p[j]);
-          else w[i][j / 8][j / 2 % 4] |= u32(__builtin_bit_cast(u16, p[j])) << (16 * (j & 1u));
-        }
-      }
-    }
   }
   if (DOWN) {
 #pragma unroll
@@ -207,8 +243,9 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 
   __shared__ u32x4_t tile[DOWN ? kMxTileRows * kMxTileBytes / 16 : 1];
   const u32 down = blockIdx.x / tiles_across;
   const u64 row0 = u64(down) * kMxTileRows, col0 = u64(blockIdx.x - down * tiles_across) * COLS;
-  if (row0 + kMxTileRows <= a.rows && col0 + COLS <= a.cols) mx_quantize_tile<TYPE, ALONG, DOWN, true>(a, row0, col0, tile);
-  else mx_quantize_tile<TYPE, ALONG, DOWN, false>(a, row0, col0, tile);
+  if (row0 + kMxTileRows <= a.rows && col0 + COLS <= a.cols) mx_quantize_tile<TYPE, ALONG, DOWN, kWholeTile>(a, row0, col0, tile);
+  else if (a.cols >= MxPack<TYPE>::kValues) mx_quantize_tile<TYPE, ALONG, DOWN, kEdgeTile>(a, row0, col0, tile);
+  else mx_quantize_tile<TYPE, ALONG, DOWN, kNarrowTile>(a, row0, col0, tile);
 }
 
 struct MxDequantizeArgs {
