@@ -24,6 +24,7 @@ import hashlib
 import json
 import math
 import os
+import re
 import sys
 import time
 
@@ -66,13 +67,19 @@ def parse():
 
 
 def source_digest():
-    """Digest of the kernel sources: ties the counter figures under profiles/ to the code they were taken on."""
+    """Digest of the sources of the kernels timed here (zc_api.hip and the headers beside it that it includes): ties the counter figures under profiles/
+    to the code they were taken on."""
     d = os.path.join(ROOT, "paper_2502_18554_amd", "csrc")
+    text, left = {}, ["zc_api.hip"]
+    while left:
+        name = left.pop()
+        if name not in text and os.path.exists(os.path.join(d, name)):
+            text[name] = open(os.path.join(d, name), "rb").read()
+            left += [n.decode() for n in re.findall(rb'#include "([^"/]+)"', text[name])]
     h = hashlib.sha256()
-    for name in sorted(os.listdir(d)):
-        if name.endswith((".h", ".hip")):
-            h.update(name.encode())
-            h.update(open(os.path.join(d, name), "rb").read())
+    for name in sorted(text):
+        h.update(name.encode())
+        h.update(text[name])
     return h.hexdigest()[:16]
 
 
