@@ -10,6 +10,11 @@
 // A value is 3 bits of fraction: by nearest rounding a second moment that changes by less than 6 % a step never
 // moves, which with b2 = 0.999 is nearly always.  So rounding is by default up or down with the probability that keeps the
 // mean, from 16 hashed bits per value and state (seed, step, place in the state).
+//
+// States in 32 bits: bound by memory (50 M values of 32 bits, gradients and copies of 16, 270 us, 5.2 TB/s, what a copy reaches; 4 groups of four values a lane, all of
+// whose loads are on their way before the first is used).  In 8 bits with weights of 32 bits as well (67 M values 205 us, 5.3 TB/s), with weights of 16 bits by arithmetic (9 M
+// values 24.9 us, 3.7 TB/s, 85 % of the vector instructions' issue time).  The tensors' table travels in the kernel's arguments, so that a step of 110 tensors is one launch that
+// nothing has to be copied for: 8 small tensors 2.3 us.
 #pragma once
 
 #include "zc_values.h"

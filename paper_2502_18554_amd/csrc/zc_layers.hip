@@ -140,7 +140,9 @@ int product(const MxProductArgs& a, hipStream_t stream) {
 
 template <int TYPE>
 int launch_quantize(const MxQuantizeArgs& a, hipStream_t stream) {
-  const u64 down = (a.rows + kMxTileRows - 1) / kMxTileRows, across = (a.cols + mx_tile_cols(TYPE) - 1) / mx_tile_cols(TYPE), tiles = down * across;
+  const bool by_columns = a.held_t.codes;
+  const u64 rows = mx_quantize_rows(by_columns), cols = mx_quantize_cols(TYPE, by_columns);
+  const u64 down = (a.rows + rows - 1) / rows, across = (a.cols + cols - 1) / cols, tiles = down * across;
   if (tiles > kMostGroups) return ZC_ERR_ARG;
   if (a.held.codes && a.held_t.codes) hipLaunchKernelGGL((mx_quantize_kernel<TYPE, true, true>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(across));
   else if (a.held.codes) hipLaunchKernelGGL((mx_quantize_kernel<TYPE, true, false>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(across));

@@ -93,13 +93,18 @@ struct MxQuantizeArgs {
   MxHeld held, held_t;          // null codes: not wanted
 };
 
-// A workgroup takes 128 rows of 256 bytes (128 values of 16 bits, 64 of 32).  Eight threads a row hold 32 bytes each and make the blocks along the row
-// from their registers, two or four of them a block.  For the blocks down the columns the tile goes through LDS: wave w takes rows 32 w .. 32 w + 31, a
-// lane one column (of 32 bits) or two (of 16).  Memory sees every value once, whichever of the two are wanted.
-// Tiles follow each other along the rows in the order of the workgroups: neighbours are read at the same time.  (Runs of tiles for each XCD, along the rows or down the columns, were slower
-// by 5 to 20 %: 8192 x 8192 in 16 bits along the rows 34 us, by runs 39; along both 50 and 52.)
-constexpr u32 kMxTileRows = 128, kMxTileBytes = 256;
-__host__ __device__ constexpr u32 mx_tile_cols(int type) { return kMxTileBytes / (type == ZC_F32 ? 4 : 2); }
+// A workgroup takes 32 KiB.  A thread holds 32 bytes of each of four rows and makes the blocks along them with its neighbours, two or four threads a block.  For the
+// blocks down the columns the tile (128 rows of 256 bytes) goes through LDS: wave w takes rows 32 w .. 32 w + 31, a lane one column (of 32 bits) or two (of 16).  Memory
+// sees every value once, whichever of the two are wanted.  Along the rows alone a tile is 32 rows of 1024 bytes, so that it writes whole lines of codes: of lines
+// that two workgroups share, each half goes to memory by itself (8192 x 8192 in 16 bits 30 us, by 256 bytes 34; 8000 x 8001 31 and 42; of 2048 bytes 30 and 29, and
+// 16384 x 16384 123 for 119).
+// Tiles follow each other along the rows in the order of the workgroups: neighbours are read at the same time.  (Runs of tiles for each XCD, along the rows or down the
+// columns, were slower by 5 to 20 %.)
+// Bound by memory: 8192 x 8192 in 16 bits along the rows 30 us (170 MB, 5.6 TB/s), along both axes 50 us (205 MB, 4.1 TB/s, with half lines down the columns); 24 x 4096 2.3 us, a launch.
+__host__ __device__ constexpr u32 mx_tile_bytes(bool down) { return down ? 256 : 1024; }
+__host__ __device__ constexpr u32 mx_quantize_rows(bool down) { return 32768 / mx_tile_bytes(down); }
+__host__ __device__ constexpr u32 mx_quantize_cols(int type, bool down) { return mx_tile_bytes(down) / (type == ZC_F32 ? 4 : 2); }
+constexpr u32 kMxTileBytes = mx_tile_bytes(true);
 
 struct __attribute__((packed, aligned(2))) MxSixteen { u32 w[4]; };
 
@@ -145,19 +150,20 @@ __device__ __forceinline__ void mx_quantize_tile(const MxQuantizeArgs& a, u64 ro
   using Pack = MxPack<TYPE>;
   constexpr bool WHOLE = EDGE == kWholeTile;
   constexpr u32 N = 2 * Pack::kValues, LANES = kBlockValues / N;          // values of a thread, of a row; threads of a block
-  const u32 tid = threadIdx.x, part = tid & 7u;
+  constexpr u32 PARTS = mx_tile_bytes(DOWN) / 32, ROWS = 256 / PARTS;     // threads of a row; rows at a time
+  const u32 tid = threadIdx.x, part = tid % PARTS, own_row = tid / PARTS;
   const u64 col = col0 + part * N;
   u32x4_t w[4][2];
 #pragma unroll
   for (u32 i = 0; i < 4; ++i) {
-    const u64 row = row0 + 32 * i + (tid >> 3);
+    const u64 row = row0 + ROWS * i + own_row;
     const One* const p = static_cast<const One*>(a.in) + (WHOLE ? row : min(row, a.rows - 1)) * a.stride;
 #pragma unroll
     for (u32 h = 0; h < 2; ++h) w[i][h] = mx_load_sixteen<TYPE, EDGE>(p, col + Pack::kValues * h, a.cols);
   }
   if (!WHOLE) {
     const int left = int(max(min(i64(a.cols) - i64(col), i64(1024)), i64(0)));
-    if (EDGE == kEdgeTile && col0 + 8 * N > a.cols) {
+    if (EDGE == kEdgeTile && col0 + PARTS * N > a.cols) {
 #pragma unroll
       for (u32 i = 0; i < 4; ++i)
 #pragma unroll
@@ -167,20 +173,20 @@ __device__ __forceinline__ void mx_quantize_tile(const MxQuantizeArgs& a, u64 ro
     for (u32 i = 0; i < 4; ++i)
 #pragma unroll
       for (u32 h = 0; h < 2; ++h) {
-        if (row0 + 32 * i + (tid >> 3) >= a.rows) w[i][h] = u32x4_t{0, 0, 0, 0};
+        if (row0 + ROWS * i + own_row >= a.rows) w[i][h] = u32x4_t{0, 0, 0, 0};
       }
   }
   if (DOWN) {
 #pragma unroll
     for (u32 i = 0; i < 4; ++i) {
-      tile[(32 * i + (tid >> 3)) * 16 + part * 2] = w[i][0];
-      tile[(32 * i + (tid >> 3)) * 16 + part * 2 + 1] = w[i][1];
+      tile[(ROWS * i + own_row) * 16 + part * 2] = w[i][0];
+      tile[(ROWS * i + own_row) * 16 + part * 2 + 1] = w[i][1];
     }
   }
   if (ALONG) {
 #pragma unroll
     for (u32 i = 0; i < 4; ++i) {
-      const u64 row = row0 + 32 * i + (tid >> 3);
+      const u64 row = row0 + ROWS * i + own_row;
       u32 top = Pack::top_value(TYPE == ZC_F32 ? max(Pack::top(w[i][0]), Pack::top(w[i][1])) : max_pairs(Pack::top(w[i][0]), Pack::top(w[i][1])));
       top = max(top, u32(__builtin_amdgcn_update_dpp(0, int(top), 0xB1, 0xf, 0xf, true)));                    // quad_perm 1 0 3 2
       if (LANES == 4) top = max(top, u32(__builtin_amdgcn_update_dpp(0, int(top), 0x4E, 0xf, 0xf, true)));    // quad_perm 2 3 0 1
@@ -239,11 +245,11 @@ __device__ __forceinline__ void mx_quantize_tile(const MxQuantizeArgs& a, u64 ro
 
 template <int TYPE, bool ALONG, bool DOWN>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(MxQuantizeArgs a, u32 tiles_across) {
-  constexpr u32 COLS = mx_tile_cols(TYPE);
-  __shared__ u32x4_t tile[DOWN ? kMxTileRows * kMxTileBytes / 16 : 1];
+  constexpr u32 ROWS = mx_quantize_rows(DOWN), COLS = mx_quantize_cols(TYPE, DOWN);
+  __shared__ u32x4_t tile[DOWN ? ROWS * kMxTileBytes / 16 : 1];
   const u32 down = blockIdx.x / tiles_across;
-  const u64 row0 = u64(down) * kMxTileRows, col0 = u64(blockIdx.x - down * tiles_across) * COLS;
-  if (row0 + kMxTileRows <= a.rows && col0 + COLS <= a.cols) mx_quantize_tile<TYPE, ALONG, DOWN, kWholeTile>(a, row0, col0, tile);
+  const u64 row0 = u64(down) * ROWS, col0 = u64(blockIdx.x - down * tiles_across) * COLS;
+  if (row0 + ROWS <= a.rows && col0 + COLS <= a.cols) mx_quantize_tile<TYPE, ALONG, DOWN, kWholeTile>(a, row0, col0, tile);
   else if (a.cols >= MxPack<TYPE>::kValues) mx_quantize_tile<TYPE, ALONG, DOWN, kEdgeTile>(a, row0, col0, tile);
   else mx_quantize_tile<TYPE, ALONG, DOWN, kNarrowTile>(a, row0, col0, tile);
 }

@@ -4,6 +4,8 @@
 // a sum's order depends on the sizes only.  A wave reads four blocks (64 bytes) of 16 rows of b with one load, and keeps the loads of a span in flight.
 // Rows of a come as they are held, or (up to 8) as values: then a lane quantises the block that it brings to the instruction, in registers: some 60 operations for
 // every four loads, mostly hidden behind them, where a launch of its own for that takes half as long as the product.
+// 1 row x 4096 x 4096 4.3 us, held 3.3 (9 MB at 2.7 TB/s; some 2 of it are a launch's, the rest two rounds of loads, for the scales and codes of a span, and the sum over the waves);
+// 24 held rows x 16384 x 4096 10.8 us (36 MB at 3.4 TB/s).
 #pragma once
 
 #include "zc_mx_product.h"
