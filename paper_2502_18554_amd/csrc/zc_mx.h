@@ -100,7 +100,8 @@ struct MxQuantizeArgs {
 // 16384 x 16384 123 for 119).
 // Tiles follow each other along the rows in the order of the workgroups: neighbours are read at the same time.  (Runs of tiles for each XCD, along the rows or down the
 // columns, were slower by 5 to 20 %.)
-// Bound by memory: 8192 x 8192 in 16 bits along the rows 30 us (170 MB, 5.6 TB/s), along both axes 50 us (205 MB, 4.1 TB/s, with half lines down the columns); 24 x 4096 2.3 us, a launch.
+// Bound by memory: 8192 x 8192 in 16 bits along the rows 30 us (170 MB, 5.6 TB/s), along both axes 50 us (205 MB, 4.1 TB/s; tiles of 256 rows, which
+// write whole lines of codes down the columns too, took as long, and small matrices 20 % longer); 24 x 4096 2.3 us, a launch.
 __host__ __device__ constexpr u32 mx_tile_bytes(bool down) { return down ? 256 : 1024; }
 __host__ __device__ constexpr u32 mx_quantize_rows(bool down) { return 32768 / mx_tile_bytes(down); }
 __host__ __device__ constexpr u32 mx_quantize_cols(int type, bool down) { return mx_tile_bytes(down) / (type == ZC_F32 ? 4 : 2); }
