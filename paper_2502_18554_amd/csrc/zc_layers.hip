@@ -65,11 +65,13 @@ void launch_tiles(const MxProductArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL((mx_tile_kernel<T, T, TYPE>), dim3(u32(down * across < at_once ? down * across : at_once)), dim3(256), 0, stream, a, u32(down), u32(across));
 }
 
-// Few rows: as many columns a workgroup as leave a workgroup for every CU.
+// Few rows: as many columns a workgroup as leave a workgroup for every CU (24 rows x 16384 x 4096 11.0 us by 64 columns, 14.3 by 16; x 8192 x 4096 7.1 by 32, 8.5 by 16; a
+// row x 8192 x 4096 5.7 and 5.3).  Where rows of values are short, every wave takes a part of a span, so that all of them share the quantising (1 x 4096 x 1000 4.1 us, 4.8
+// by spans); of held rows a wave takes whole spans (1 x 4096 x 1024 2.4 us, 2.9 by parts).
 template <int RG, int CG, int X>
 int launch_few(MxFewArgs a, hipStream_t stream) {
   const u64 groups = (a.p.n + 16 * CG - 1) / (16 * CG), steps = (a.p.blocks + 3) / 4;
-  a.steps = steps >= 4 * kFewWaves ? 4 : steps >= 2 * kFewWaves ? 2 : 1;
+  a.steps = X == kHeldRows || steps >= 4 * kFewWaves ? 4 : steps >= 2 * kFewWaves ? 2 : 1;
   const bool whole = a.steps == 4 && a.p.blocks % kSpanOfBlocks == 0 && (X == kHeldRows || a.k % kBlockValues == 0);
   if (whole) hipLaunchKernelGGL((mx_few_kernel<RG, CG, X, true>), dim3(u32(groups)), dim3(64 * kFewWaves), 0, stream, a);
   else hipLaunchKernelGGL((mx_few_kernel<RG, CG, X, false>), dim3(u32(groups)), dim3(64 * kFewWaves), 0, stream, a);

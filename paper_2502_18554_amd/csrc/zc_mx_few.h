@@ -20,7 +20,7 @@ struct MxFewArgs {
   MxProductArgs p;               // (without a where the rows come as values)
   const void* x;
   u64 x_stride, k;
-  u32 steps;                     // of four blocks that a wave takes in turn: 4 (a span), 2 or 1
+  u32 steps;                     // of four blocks that a wave takes in turn where the rows come as values: 4 (a span), 2 or 1
 };
 
 // What a lane brings of a: a block of a row as it comes, and then as codes with its scale byte.
@@ -105,6 +105,7 @@ template <int RG, int CG, int X, bool WHOLE>
 __global__ __launch_bounds__(64 * kFewWaves) void mx_few_kernel(MxFewArgs a) {
   // Steps whose values of a are on their way together: as many as leave room for b's.
   constexpr u32 AHEAD = X == kHeldRows ? 4 : 64 / (RG * (X == ZC_F32 ? 32 : 16));
+  constexpr bool SPANS = WHOLE || X == kHeldRows;       // a wave takes whole spans
   __shared__ f32x4_t parts[kFewWaves * RG * CG * 64];
   const u32 lane = threadIdx.x & 63u, wave = u32(__builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6))), in16 = lane & 15u, part = lane >> 4;
   const u64 col0 = u64(blockIdx.x) * (16 * CG);
@@ -129,8 +130,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx_few_kernel(MxFewArgs a) {
   for (int r = 0; r < RG; ++r)
 #pragma unroll
     for (int c = 0; c < CG; ++c) sum[r][c] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-  for (u32 turn = wave * (WHOLE ? 4u : a.steps); 4 * turn < a.p.blocks; turn += kFewWaves * (WHOLE ? 4u : a.steps)) {
-    const u32 first = turn / 4 * kSpanOfBlocks, t0 = WHOLE ? 0u : turn & 3u, t1 = WHOLE ? 4u : t0 + a.steps;             // the span, and the steps of it that are this wave's
+  for (u32 turn = wave * (SPANS ? 4u : a.steps); 4 * turn < a.p.blocks; turn += kFewWaves * (SPANS ? 4u : a.steps)) {
+    const u32 first = turn / 4 * kSpanOfBlocks, t0 = SPANS ? 0u : turn & 3u, t1 = SPANS ? 4u : t0 + a.steps;             // the span, and the steps of it that are this wave's
     u32x4_t b[CG][4], sb[CG], sa[RG];
     MxRaw<X> x[RG][AHEAD];
     const auto load_x = [&](u32 from) {
