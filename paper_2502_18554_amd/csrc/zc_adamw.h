@@ -1,7 +1,7 @@
 // One AdamW step over many tensors in one launch, with first and second moments in 32 bits or in 8.
 //
-// For every value (all steps in binary32, each rounded by itself, except that the quotient, and the root where it is not stored, are within
-// a unit in the last place; c.* come from binary64 on the host):
+// For every value (all steps in binary32, each rounded by itself, except that the quotient is a product with the reciprocal instruction's result, within
+// three units in the last place; c.* come from binary64 on the host):
 //   g = grad x scale;  m' = b1 m + (1 - b1) g;  v' = b2 v + ((1 - b2) g) g;  r = sqrt(v')
 //   p' = p (1 - lr decay) - (lr / (1 - b1^t)) (m' / (r / sqrt(1 - b2^t) + eps))
 // In 8 bits a state holds m and r (the root: half the exponent range of v) as e4m3 codes, 32 values a block, the stream
@@ -208,7 +208,7 @@ __device__ __forceinline__ void adamw_tile(const AdamwArgs& a, const AdamwEntry&
       g[j] = float(raw_g[u].v[j]) * scale;
       m[j] = m[j] * c.b1 + g[j] * c.c1;
       v[j] = v[j] * c.b2 + (g[j] * c.c2) * g[j];
-      r[j] = BITS == 8 ? sqrtf(v[j]) : __builtin_amdgcn_sqrtf(v[j]);
+      r[j] = sqrtf(v[j]);                                            // (the instruction by itself takes subnormal values for zeros)
       p[j] = p[j] * c.keep - (m[j] * __builtin_amdgcn_rcpf(r[j] * c.root + c.eps)) * c.rate;
     }
     if (WHOLE || i + 4 <= x.n) {

@@ -202,9 +202,13 @@ int zc_adamw(int k, const size_t* n, void* const* d_params, int param_type, cons
   a.c.b2 = float(beta2);
   a.c.c2 = float(1 - beta2);
   a.c.keep = float(1 - lr * weight_decay);
-  a.c.rate = float(lr / (1 - std::pow(beta1, double(step))));
-  a.c.root = float(1 / std::sqrt(1 - std::pow(beta2, double(step))));
-  a.c.eps = float(eps);
+  // The reciprocal instruction takes subnormal numbers for zeros and makes none.  A denominator is eps, or at least a root, 2^-75, and at most 2^91 and eps: where eps lets it
+  // be subnormal, or so large that its reciprocal is, it is scaled by a power of two (exactly), which the last factor takes out again.
+  const float eps32 = float(eps);
+  const double scaled = eps32 > 0 && eps32 < 0x1p-126f ? 0x1p24 : eps32 >= 0x1p96f ? 0x1p-32 : 1;
+  a.c.rate = float(lr / (1 - std::pow(beta1, double(step))) * scaled);
+  a.c.root = float(1 / std::sqrt(1 - std::pow(beta2, double(step))) * scaled);
+  a.c.eps = float(double(eps32) * scaled);
   a.copy_type = copy_type;
   a.state = static_cast<u8*>(d_state);
   a.blocks = blocks;
