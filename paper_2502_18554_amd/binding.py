@@ -421,6 +421,11 @@ def _one_type(tensors):
     return _TYPES.get(kinds.pop(), -1) if len(kinds) == 1 else ZC_F32 if not kinds else -1
 
 
+def _own_bytes(t):
+    """Whether a state or a workspace is None or on the GPU in one piece: of a tensor with strides the bytes lie elsewhere, or are not all there."""
+    return t is None or (t.is_cuda and t.is_contiguous())
+
+
 def zc_adamw(d_params, d_grads, d_state, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, state_bits=32, seed=0, d_copies=None,
              d_grad_scale=None, stream=None):
     """One AdamW step over the tensors of the list d_params (contiguous, of one type; d_grads: as many of the same sizes, of one type), in place.
@@ -437,7 +442,7 @@ def zc_adamw(d_params, d_grads, d_state, step, lr, beta1=0.9, beta2=0.999, eps=1
     sizes = [t.numel() for t in d_params]
     if [t.numel() for t in d_grads] != sizes or not all(t.is_contiguous() and t.is_cuda for t in (*d_params, *d_grads, *copies)) or \
             any(t is not None and t.numel() != n for t, n in zip(d_copies or (), sizes)) or \
-            not all(t is None or t.is_cuda for t in (d_state, d_grad_scale)) or (d_grad_scale is not None and (d_grad_scale.dtype != torch.float32 or d_grad_scale.numel() != 1)):
+            not _own_bytes(d_state) or not (d_grad_scale is None or d_grad_scale.is_cuda) or (d_grad_scale is not None and (d_grad_scale.dtype != torch.float32 or d_grad_scale.numel() != 1)):
         return ZC_ERR_ARG
     lists = [_words(sizes), _words([t.data_ptr() for t in d_params]), _words([t.data_ptr() for t in d_grads]),
              _words([t.data_ptr() if t is not None else 0 for t in d_copies]) if d_copies is not None else (None, None)]
@@ -548,7 +553,7 @@ def zc_mx_product(d_a_codes, d_a_scales, d_b_codes, d_b_scales, k, d_out, d_ws, 
     k = int(k)
     end = _product_end(d_b_codes, d_b_scales, k, d_out, d_bias)
     a = end and _held(d_a_codes, d_a_scales, end[0][2])
-    if not a or not _covers(d_a_codes, d_a_scales, k) or not (d_ws is None or d_ws.is_cuda):
+    if not a or not _covers(d_a_codes, d_a_scales, k) or not _own_bytes(d_ws):
         return ZC_ERR_ARG
     out, b = end
     return lib().zc_mx_product(*a, *b, out[2], out[3], k, _p(d_bias), out[0], out[1], out[4], ZC_MX_ADD if add else 0, _p(d_ws),
@@ -565,7 +570,7 @@ def zc_mx_linear(d_x, d_w_codes, d_w_scales, d_out, d_ws, d_bias=None, add=False
             return r
     x = _matrix(d_x)
     end = x and _product_end(d_w_codes, d_w_scales, x[3], d_out, d_bias)
-    if not end or end[0][2] != x[2] or not (d_ws is None or d_ws.is_cuda):
+    if not end or end[0][2] != x[2] or not _own_bytes(d_ws):
         return ZC_ERR_ARG
     out, w = end
     return lib().zc_mx_linear(x[0], x[1], x[4], *w, out[2], out[3], x[3], _p(d_bias), out[0], out[1], out[4], ZC_MX_ADD if add else 0, _p(d_ws),

@@ -87,9 +87,10 @@ bool bias_of(PyObject* o, size_t n, const float*& p) {
   p = static_cast<const float*>(t->data_ptr());
   return true;
 }
+// A state or a workspace.
 bool workspace_of(PyObject* o, void*& p, size_t& bytes) {
   const at::Tensor* const t = tensor(o);
-  if (!t) return false;
+  if (!t || !t->is_contiguous()) return false;           // (its bytes are not all its own, or not all there, otherwise)
   p = t->data_ptr();
   bytes = t->nbytes();
   return true;

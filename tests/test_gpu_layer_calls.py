@@ -1,0 +1,55 @@
+"""The layer calls' way from tensors to the library: by native code and by ctypes alike, the same refusals and the same results."""
+import pytest
+import torch
+
+import paper_2502_18554_amd as zc
+from paper_2502_18554_amd import binding as b
+from paper_2502_18554_amd.binding import ZC_ERR_ARG, ZC_OK
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+@pytest.fixture(params=["native", "ctypes"])
+def way(request, monkeypatch):
+    b.lib()
+    if request.param == "ctypes":
+        monkeypatch.setattr(b, "_native_layers", None)
+    elif b._native_layers is None:
+        pytest.skip("the native calls are not built")
+    return request.param
+
+
+def room(rows, cols, fill=0):
+    return (torch.full((rows, zc.zc_mx_codes_stride(cols)), fill, dtype=torch.uint8, device=DEV),
+            torch.full((rows, zc.zc_mx_scales_stride(cols)), fill, dtype=torch.uint8, device=DEV))
+
+
+def in_pieces(nbytes):
+    """Tensors that say they have so many bytes: every second one of a buffer's, one byte, or one row, again and again, and a buffer across."""
+    wide = torch.zeros(2 * nbytes, dtype=torch.uint8, device=DEV)
+    return [wide[::2], wide[:1].expand(nbytes), wide[:16].expand(-(-nbytes // 16), 16), wide.view(2, nbytes).t()]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_states_in_pieces_are_refused(way, bits):
+    p, g = torch.ones(100, device=DEV), torch.ones(100, device=DEV)
+    for state in in_pieces(zc.zc_adamw_state_bytes([100], bits)):
+        assert state.nbytes >= zc.zc_adamw_state_bytes([100], bits) and not state.is_contiguous()
+        assert zc.zc_adamw([p], [g], state, 1, 1e-3, state_bits=bits) == ZC_ERR_ARG
+    torch.cuda.synchronize()
+    assert (p == 1).all()
+
+
+@pytest.mark.parametrize("m", [4, 40])
+def test_workspaces_in_pieces_are_refused(way, m):
+    n, k = 48, 200
+    x, w, a = torch.ones(m, k, device=DEV), room(n, k, 0x22), room(m, k, 0x22)
+    out = torch.full((m, n), 5.0, device=DEV)
+    for ws in in_pieces(zc.zc_mx_workspace_bytes(m, n, k)):
+        assert zc.zc_mx_linear(x, *w, out, ws) == ZC_ERR_ARG
+        assert zc.zc_mx_product(*a, *w, k, out, ws) == ZC_ERR_ARG
+    torch.cuda.synchronize()
+    assert (out == 5).all()
+    assert zc.zc_mx_linear(x, *w, out, torch.empty(zc.zc_mx_workspace_bytes(m, n, k), dtype=torch.uint8, device=DEV)) == ZC_OK
