@@ -490,7 +490,7 @@ def _held(codes, scales, rows):
 def _covers(codes, scales, cols):
     """Whether rows of codes and scale bytes have room for so many values."""
     blocks = -(-cols // 32)
-    return codes.shape[1] >= 16 * blocks and scales.shape[1] >= blocks
+    return codes.dim() == scales.dim() == 2 and codes.shape[1] >= 16 * blocks and scales.shape[1] >= blocks
 
 
 def zc_mx_quantize(d_in, d_codes, d_scales, d_codes_t=None, d_scales_t=None, stream=None):

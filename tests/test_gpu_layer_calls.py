@@ -53,3 +53,19 @@ def test_workspaces_in_pieces_are_refused(way, m):
     torch.cuda.synchronize()
     assert (out == 5).all()
     assert zc.zc_mx_linear(x, *w, out, torch.empty(zc.zc_mx_workspace_bytes(m, n, k), dtype=torch.uint8, device=DEV)) == ZC_OK
+
+
+def test_codes_and_scales_that_are_no_matrices_are_refused(way):
+    m, n, k = 8, 16, 64
+    x, a, w, out = torch.zeros(m, k, device=DEV), room(m, k), room(n, k), torch.zeros(m, n, device=DEV)
+    ws = torch.empty(zc.zc_mx_workspace_bytes(m, n, k), dtype=torch.uint8, device=DEV)
+    for i in range(2):
+        for change in (lambda t: t[0], lambda t: t[None], lambda t: t.view(-1), lambda t: t[0, 0]):
+            flat, flat_w = list(a), list(w)
+            flat[i], flat_w[i] = change(a[i]), change(w[i])
+            assert zc.zc_mx_quantize(x, *flat) == ZC_ERR_ARG
+            assert zc.zc_mx_quantize(x, None, None, *flat) == ZC_ERR_ARG
+            assert zc.zc_mx_dequantize(*flat, x) == ZC_ERR_ARG
+            assert zc.zc_mx_product(*flat, *w, k, out, ws) == ZC_ERR_ARG
+            assert zc.zc_mx_product(*a, *flat_w, k, out, ws) == ZC_ERR_ARG
+            assert zc.zc_mx_linear(x, *flat_w, out, ws) == ZC_ERR_ARG
