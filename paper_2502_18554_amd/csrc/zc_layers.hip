@@ -140,15 +140,34 @@ int product(const MxProductArgs& a, hipStream_t stream) {
   return by_columns(a, [&](const MxProductArgs& part) { return product_launch(part, stream); });
 }
 
+MxHeld from_block(MxHeld h, u64 row, u64 block) {
+  if (!h.codes) return h;
+  h.codes += row * h.codes_stride + kMxBytes * block;
+  h.scales += row * h.scales_stride + block;
+  return h;
+}
+
 template <int TYPE>
 int launch_quantize(const MxQuantizeArgs& a, hipStream_t stream) {
   const bool by_columns = a.held_t.codes;
   const u64 rows = mx_quantize_rows(by_columns), cols = mx_quantize_cols(TYPE, by_columns);
-  const u64 down = (a.rows + rows - 1) / rows, across = (a.cols + cols - 1) / cols, tiles = down * across;
-  if (tiles > kMostGroups) return ZC_ERR_ARG;
-  if (a.held.codes && a.held_t.codes) hipLaunchKernelGGL((mx_quantize_kernel<TYPE, true, true>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(across));
-  else if (a.held.codes) hipLaunchKernelGGL((mx_quantize_kernel<TYPE, true, false>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(across));
-  else hipLaunchKernelGGL((mx_quantize_kernel<TYPE, false, true>), dim3(u32(tiles)), dim3(256), 0, stream, a, u32(across));
+  // Pieces of whole tiles, as many as a grid counts (long thin matrices have more: 2^30 values of 32 bits down the columns of one row are 2^24 tiles).
+  const u64 most_cols = kMostGroups * cols;
+  for (u64 col = 0; col < a.cols; col += most_cols) {
+    const u64 now = a.cols - col < most_cols ? a.cols - col : most_cols, across = (now + cols - 1) / cols, most_rows = kMostGroups / across * rows;
+    for (u64 row = 0; row < a.rows; row += most_rows) {
+      MxQuantizeArgs part = a;
+      part.rows = a.rows - row < most_rows ? a.rows - row : most_rows;
+      part.cols = now;
+      part.in = static_cast<const u8*>(a.in) + (row * a.stride + col) * value_bytes(TYPE);
+      part.held = from_block(a.held, row, col / kBlockValues);
+      part.held_t = from_block(a.held_t, col, row / kBlockValues);
+      const u32 tiles = u32((part.rows + rows - 1) / rows * across);
+      if (a.held.codes && a.held_t.codes) hipLaunchKernelGGL((mx_quantize_kernel<TYPE, true, true>), dim3(tiles), dim3(256), 0, stream, part, u32(across));
+      else if (a.held.codes) hipLaunchKernelGGL((mx_quantize_kernel<TYPE, true, false>), dim3(tiles), dim3(256), 0, stream, part, u32(across));
+      else hipLaunchKernelGGL((mx_quantize_kernel<TYPE, false, true>), dim3(tiles), dim3(256), 0, stream, part, u32(across));
+    }
+  }
   return launched();
 }
 int quantize(const MxQuantizeArgs& a, hipStream_t stream) {
