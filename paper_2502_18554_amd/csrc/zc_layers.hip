@@ -57,6 +57,7 @@ bool matrix_valid(const void* p, int type, u64 rows, u64 cols, u64 stride) {
   return type_valid(type) && stride >= cols && stride <= (u64(1) << 32) && (rows == 0 || cols == 0 || (p && aligned(p, value_bytes(type))));
 }
 bool sizes_valid(u64 rows, u64 cols) { return rows <= 0x7fffffffu && cols <= 0x7fffffffu; }
+bool product_valid(u64 m, u64 n, u64 k) { return sizes_valid(m, k) && sizes_valid(n, k) && ((m + 63) / 64) * ((n + 63) / 64) <= kMostTiles; }
 
 template <int T, int TYPE>
 void launch_tiles(const MxProductArgs& a, hipStream_t stream) {
@@ -136,7 +137,6 @@ int product_launch(const MxProductArgs& a, hipStream_t stream) {
 }
 int product(const MxProductArgs& a, hipStream_t stream) {
   if (a.m == 0 || a.n == 0) return ZC_OK;
-  if (((a.m + 63) / 64) * ((a.n + 63) / 64) > kMostTiles) return ZC_ERR_ARG;
   return by_columns(a, [&](const MxProductArgs& part) { return product_launch(part, stream); });
 }
 
@@ -307,7 +307,7 @@ int zc_mx_dequantize(const void* d_codes, size_t codes_stride, const void* d_sca
 int zc_mx_product(const void* d_a, size_t a_stride, const void* d_a_scales, size_t a_scales_stride, const void* d_b, size_t b_stride,
                   const void* d_b_scales, size_t b_scales_stride, size_t m, size_t n, size_t k, const float* d_bias, void* d_out, int out_type,
                   size_t out_stride, unsigned flags, void* d_ws, size_t ws_bytes, void* hip_stream) {
-  if (!sizes_valid(m, k) || !sizes_valid(n, k) || (flags & ~ZC_MX_ADD) || !matrix_valid(d_out, out_type, m, n, out_stride)) return ZC_ERR_ARG;
+  if (!product_valid(m, n, k) || (flags & ~ZC_MX_ADD) || !matrix_valid(d_out, out_type, m, n, out_stride)) return ZC_ERR_ARG;
   if (!held_valid(d_a, d_a_scales, m, k, a_stride, a_scales_stride) || !held_valid(d_b, d_b_scales, n, k, b_stride, b_scales_stride)) return ZC_ERR_ARG;
   if (!aligned(d_bias, 4) || !aligned(d_ws, 16)) return ZC_ERR_ARG;
   (void)ws_bytes;
@@ -334,7 +334,7 @@ int zc_mx_linear(const void* d_x, int x_type, size_t x_stride, const void* d_w, 
   u8* const codes = static_cast<u8*>(d_ws);
   u8* const scales = codes + codes_bytes;
   // (the product's own checks come first: nothing is launched by a call that is refused)
-  if (!sizes_valid(n, k) || (flags & ~ZC_MX_ADD) || !matrix_valid(d_out, out_type, m, n, out_stride) || !aligned(d_bias, 4) ||
+  if (!product_valid(m, n, k) || (flags & ~ZC_MX_ADD) || !matrix_valid(d_out, out_type, m, n, out_stride) || !aligned(d_bias, 4) ||
       !held_valid(d_w, d_w_scales, n, k, w_stride, w_scales_stride))
     return ZC_ERR_ARG;
   if (m == 0 || n == 0) return ZC_OK;

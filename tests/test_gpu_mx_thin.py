@@ -5,7 +5,7 @@ import torch
 
 import layers_model as model
 import paper_2502_18554_amd as zc
-from paper_2502_18554_amd.binding import ZC_OK
+from paper_2502_18554_amd.binding import ZC_ERR_ARG, ZC_OK
 
 pytestmark = pytest.mark.gpu
 
@@ -83,3 +83,14 @@ def test_a_layer_on_as_many_rows():
     at = places(m, [MOST * 32])
     want = 3 * model.mx_values(*model.mx_quantize(x[at].float().cpu().numpy()), 1)
     assert np.array_equal(out[at].double().cpu().numpy(), want)
+
+
+def test_a_layer_with_too_many_results_launches_nothing():
+    """More results than a product counts (their memory does not exist: the call is refused ahead of them)."""
+    m, n, k = 4160, (1 << 31) - 1, 32
+    x = torch.ones((m, k), device=DEV)
+    ws = torch.full((zc.zc_mx_workspace_bytes(m, n, k),), 0xA5, dtype=torch.uint8, device=DEV)
+    some = ws.data_ptr()
+    assert zc.binding.lib().zc_mx_linear(x.data_ptr(), 0, k, some, 16, some, 4, m, n, k, None, some, 0, n, 0, ws.data_ptr(), ws.nbytes, None) == ZC_ERR_ARG
+    torch.cuda.synchronize()
+    assert (ws == 0xA5).all()
