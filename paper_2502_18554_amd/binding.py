@@ -100,26 +100,38 @@ def lib():
     return _lib
 
 
+def _module(name):
+    """A module of native calls that was built for this Python, or None: ctypes takes its calls then."""
+    path = os.path.join(_HERE, name + sysconfig.get_config_var("EXT_SUFFIX"))
+    if not os.path.exists(path):
+        return None
+    try:
+        spec = importlib.util.spec_from_file_location(name, path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError:              # one that does not load
+        return None
+    return module
+
+
 def _load_native(L):
     global _native, _native_layers
-    path = os.path.join(_HERE, "_zc_calls" + sysconfig.get_config_var("EXT_SUFFIX"))      # (the one that was built for this Python)
     stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if not os.path.exists(path) or stream_of is None:
-        return
-    try:
-        spec = importlib.util.spec_from_file_location("_zc_calls", path)
-        native = importlib.util.module_from_spec(spec)
-        spec.loader.exec_module(native)
-    except ImportError:              # one that does not load: ctypes takes all calls
+    native = _module("_zc_calls") if stream_of is not None else None
+    if native is None:
         return
     calls = (L.zc_compress_ex, L.zc_decompress_ex, L.zc_reduce_compressed_op, L.zc_reduce_step_op, L.zc_decompress_many)
     native.setup(*(C.cast(f, C.c_void_p).value for f in calls), torch._C._cuda_getDevice, stream_of)
     _native = native
-    setup = getattr(native, "setup_layers", None)
-    if setup:
-        calls = (L.zc_adamw, L.zc_mx_quantize, L.zc_mx_dequantize, L.zc_mx_product, L.zc_mx_linear)
-        if setup(*(C.cast(f, C.c_void_p).value for f in calls), str(torch.__version__).split("+")[0]):
-            _native_layers = native
+    layers = _module("_zc_layer_calls")
+    if layers is None:
+        return
+    for name in ("setup_layers", "adamw", "quantize", "dequantize", "product", "linear"):      # (the native calls in one place)
+        setattr(native, name, getattr(layers, name))
+    layers.setup_streams(torch._C._cuda_getDevice, stream_of)
+    calls = (L.zc_adamw, L.zc_mx_quantize, L.zc_mx_dequantize, L.zc_mx_product, L.zc_mx_linear)
+    if layers.setup_layers(*(C.cast(f, C.c_void_p).value for f in calls), str(torch.__version__).split("+")[0]):
+        _native_layers = layers
 
 
 # Small calls are bound by what happens here (a chunk of a few thousand values runs for 4 us).  Where ctypes takes a call, addresses go to

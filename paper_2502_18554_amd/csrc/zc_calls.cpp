@@ -12,6 +12,7 @@
 #include <cstdint>
 
 #include "../../include/zc.h"
+#include "zc_calls_stream.h"
 
 namespace {
 
@@ -22,8 +23,8 @@ struct Calls {
   decltype(&zc_reduce_step_op) step;
   decltype(&zc_decompress_many) many;
 } g_calls;
-PyObject *g_device, *g_raw_stream;             // torch's own: the current device, and the current stream's handle on a device
-PyObject *g_data_ptr, *g_nbytes, *g_numel, *g_cuda_stream;     // names
+zc_calls::Streams g_streams;
+PyObject *g_data_ptr, *g_nbytes, *g_numel;     // names
 
 // Every reader below returns false where the object is not of a plain form (nothing raised), or with an exception set.
 bool exact(PyObject* o, uint64_t& v) {
@@ -94,32 +95,7 @@ bool own_capacity(PyObject* given, PyObject* tensor, bool elements, uint64_t& v)
   return tensor == Py_None || of_method(tensor, g_numel, v);
 }
 
-}  // namespace
-
-namespace zc_calls {
-PyMethodDef* layer_methods() __attribute__((weak));      // zc_layer_calls.cpp, where it is built along
-// The stream as given, or the current one.
-bool stream_of(PyObject* given, void*& stream) {
-  uint64_t v = 0;
-  if (given != Py_None) {
-    if (!of_attribute(given, g_cuda_stream, v)) return false;
-    stream = reinterpret_cast<void*>(v);
-    return true;
-  }
-  PyObject* device = PyObject_CallNoArgs(g_device);
-  if (!device) return false;
-  PyObject* r = PyObject_CallOneArg(g_raw_stream, device);
-  Py_DECREF(device);
-  if (!r) return false;
-  const bool ok = exact(r, v);
-  Py_DECREF(r);
-  stream = reinterpret_cast<void*>(v);
-  return ok;
-}
-}  // namespace zc_calls
-
-namespace {
-using zc_calls::stream_of;
+bool stream_of(PyObject* given, void*& stream) { return g_streams.of(given, stream); }
 
 PyObject* not_this_way() {
   if (PyErr_Occurred()) return nullptr;
@@ -312,12 +288,7 @@ PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   g_calls.reduce = reinterpret_cast<decltype(g_calls.reduce)>(at[2]);
   g_calls.step = reinterpret_cast<decltype(g_calls.step)>(at[3]);
   g_calls.many = reinterpret_cast<decltype(g_calls.many)>(at[4]);
-  PyObject* const device = g_device;
-  PyObject* const raw = g_raw_stream;
-  g_device = Py_NewRef(a[5]);
-  g_raw_stream = Py_NewRef(a[6]);
-  Py_XDECREF(device);
-  Py_XDECREF(raw);
+  g_streams.set(a[5], a[6]);
   Py_RETURN_NONE;
 }
 
@@ -334,12 +305,7 @@ PyMODINIT_FUNC PyInit__zc_calls() {
   g_data_ptr = PyUnicode_InternFromString("data_ptr");
   g_nbytes = PyUnicode_InternFromString("nbytes");
   g_numel = PyUnicode_InternFromString("numel");
-  g_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-  if (!g_data_ptr || !g_nbytes || !g_numel || !g_cuda_stream) return nullptr;
-  PyObject* const module = PyModule_Create(&g_module);
-  if (module && zc_calls::layer_methods && PyModule_AddFunctions(module, zc_calls::layer_methods()) < 0) {
-    Py_DECREF(module);
-    return nullptr;
-  }
-  return module;
+  g_streams.cuda_stream = PyUnicode_InternFromString("cuda_stream");
+  if (!g_data_ptr || !g_nbytes || !g_numel || !g_streams.cuda_stream) return nullptr;
+  return PyModule_Create(&g_module);
 }

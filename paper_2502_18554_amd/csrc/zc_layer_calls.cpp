@@ -2,7 +2,8 @@
 //
 // A step over a list of tensors asks each of them for address, size, type and layout.  From Python, or through Python's attributes, that is 0.4 to 0.8 us a
 // tensor, more than the step itself takes on small ones; here the tensors are read as what they are, 20 ns each.  That needs the headers
-// of torch, and the module is only used with the torch that it was built for.
+// of torch and its libraries: this is a module of its own, which is only used with the torch that it was built for; without it these calls go through ctypes, and the
+// codec's native calls (zc_calls.cpp) are as they were.
 // Nothing is decided here: what is not of a plain form, or does not fit together, is answered with NotImplemented, and binding.py takes the call its own way.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -14,12 +15,12 @@
 #include <vector>
 
 #include "../../include/zc.h"
-
-namespace zc_calls {
-bool stream_of(PyObject* given, void*& stream);      // (zc_calls.cpp)
-}
+#include "zc_calls_stream.h"
 
 namespace {
+
+zc_calls::Streams g_streams;
+bool stream_of(PyObject* given, void*& stream) { return g_streams.of(given, stream); }
 
 struct Calls {
   decltype(&zc_adamw) adamw;
@@ -106,7 +107,7 @@ PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   if (n_args != 6 || !matrix(a[0], x)) return not_this_way();
   if ((a[1] != Py_None || a[2] != Py_None) && !held(a[1], a[2], x.rows, x.cols, h)) return not_this_way();
   if ((a[3] != Py_None || a[4] != Py_None) && !held(a[3], a[4], x.cols, x.rows, ht)) return not_this_way();
-  if (!zc_calls::stream_of(a[5], stream)) return not_this_way();
+  if (!stream_of(a[5], stream)) return not_this_way();
   int st;
   Py_BEGIN_ALLOW_THREADS
   st = g_calls.quantize(x.at, x.type, x.rows, x.cols, x.stride, h.codes, h.codes_stride, h.scales, h.scales_stride, ht.codes, ht.codes_stride, ht.scales, ht.scales_stride, stream);
@@ -119,7 +120,7 @@ PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   Matrix out;
   Held h;
   void* stream;
-  if (n_args != 4 || !matrix(a[2], out) || !held(a[0], a[1], out.rows, out.cols, h) || !zc_calls::stream_of(a[3], stream)) return not_this_way();
+  if (n_args != 4 || !matrix(a[2], out) || !held(a[0], a[1], out.rows, out.cols, h) || !stream_of(a[3], stream)) return not_this_way();
   int st;
   Py_BEGIN_ALLOW_THREADS
   st = g_calls.dequantize(h.codes, h.codes_stride, h.scales, h.scales_stride, out.rows, out.cols, out.at, out.type, out.stride, stream);
@@ -141,7 +142,7 @@ PyObject* product(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     return not_this_way();
   }
   if (!matrix(a[5], out) || !held(a[0], a[1], out.rows, size_t(k), x) || !held(a[2], a[3], out.cols, size_t(k), w) || !workspace_of(a[6], ws, ws_bytes) ||
-      !bias_of(a[7], out.cols, bias) || !zc_calls::stream_of(a[9], stream))
+      !bias_of(a[7], out.cols, bias) || !stream_of(a[9], stream))
     return not_this_way();
   const int add = PyObject_IsTrue(a[8]);
   if (add < 0) return nullptr;
@@ -161,7 +162,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   void *ws, *stream;
   size_t ws_bytes;
   if (n_args != 8 || !matrix(a[0], x) || !matrix(a[3], out) || out.rows != x.rows || !held(a[1], a[2], out.cols, x.cols, w) || !workspace_of(a[4], ws, ws_bytes) ||
-      !bias_of(a[5], out.cols, bias) || !zc_calls::stream_of(a[7], stream))
+      !bias_of(a[5], out.cols, bias) || !stream_of(a[7], stream))
     return not_this_way();
   const int add = PyObject_IsTrue(a[6]);
   if (add < 0) return nullptr;
@@ -220,7 +221,7 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const bool copies = a[11] != Py_None;
   if (!list_of(a[0], k, false, sizes, at.data(), types[0]) || !list_of(a[1], k, true, sizes, at.data() + k, types[1]) ||
       (copies && !list_of(a[11], k, true, sizes, at.data() + 2 * k, types[2])) || !workspace_of(a[2], state, state_bytes) || !bias_of(a[12], 1, scale) ||
-      !zc_calls::stream_of(a[13], stream))
+      !stream_of(a[13], stream))
     return not_this_way();
   int st;
   Py_BEGIN_ALLOW_THREADS
@@ -251,6 +252,16 @@ PyObject* setup_layers(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   Py_RETURN_TRUE;
 }
 
+// (torch's current device, its raw current stream)
+PyObject* setup_streams(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 2) {
+    PyErr_SetString(PyExc_TypeError, "setup_streams takes two functions");
+    return nullptr;
+  }
+  g_streams.set(a[0], a[1]);
+  Py_RETURN_NONE;
+}
+
 // (A tensor without memory of its own throws when it is asked for its address, and a list may be too long for the memory that is left.)
 using Call = PyObject*(PyObject*, PyObject* const*, Py_ssize_t);
 template <Call* F>
@@ -266,11 +277,13 @@ PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&caught<F>)), METH_FASTCALL, nullptr};
 }
 
-PyMethodDef g_methods[] = {method<setup_layers>("setup_layers"), method<adamw>("adamw"), method<quantize>("quantize"), method<dequantize>("dequantize"),
-                           method<product>("product"), method<linear>("linear"), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef g_methods[] = {method<setup_layers>("setup_layers"), method<setup_streams>("setup_streams"), method<adamw>("adamw"), method<quantize>("quantize"),
+                           method<dequantize>("dequantize"), method<product>("product"), method<linear>("linear"), {nullptr, nullptr, 0, nullptr}};
+PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_zc_layer_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
-namespace zc_calls {
-PyMethodDef* layer_methods() { return g_methods; }
-}  // namespace zc_calls
+PyMODINIT_FUNC PyInit__zc_layer_calls() {
+  g_streams.cuda_stream = PyUnicode_InternFromString("cuda_stream");
+  return g_streams.cuda_stream ? PyModule_Create(&g_module) : nullptr;
+}
