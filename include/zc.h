@@ -314,7 +314,7 @@ int zc_quality(const float* d_ref, const float* d_test, size_t n, double* out4,
 
 /* One AdamW step over k tensors of n[i] values (any count; host arrays of k entries), in as few launches as their table allows
  * (one for every 110 tensors, or 2^31 values of one).  For every value, in binary32, each operation rounded (the quotient to
- * within three units in the last place), at all magnitudes, subnormal ones among them:
+ * within three units in the last place, the root where the state holds v to within one), at all magnitudes, subnormal ones among them:
  *   g = grad x *d_grad_scale;  m' = beta1 m + (1 - beta1) g;  v' = beta2 v + ((1 - beta2) g) g;  r = sqrt(v')
  *   p' = p (1 - lr weight_decay) - (m' / (r / sqrt(1 - beta2^step) + eps)) (lr / (1 - beta1^step))
  * d_params: updated in place; d_grads: read; param_type, grad_type: ZC_F32, ZC_BF16 or ZC_F16.  d_copies (may be NULL, as may its

@@ -111,7 +111,8 @@ struct MxRows {
 };
 constexpr u64 kMostTileStride = u64(1) << 23;       // (256 rows are less than 2^32 bytes)
 
-// 16 bytes a lane to LDS, at `to` and on.  (Written out: of its own loads to LDS the compiler thinks that any read of LDS may have to wait for them.)
+// 16 bytes a lane to LDS, at `to` and on.  (Written out: of its own loads to LDS the compiler thinks that any read of LDS may have to wait for them.  m0 is reserved, so
+// that it cannot be named among what is overwritten: nothing else in these kernels may use it, as another load to LDS, a message or an indexed register would.)
 __device__ inline void mx_load_to_lds(__amdgpu_buffer_rsrc_t from, u32 to, u32 lane_offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(lane_offset), "s"(from) : "memory");
 }
