@@ -306,7 +306,7 @@ int zc_quality(const float* d_ref, const float* d_test, size_t n, double* out4,
 /* ---- The calls around the collective: the optimiser's step that takes the averaged gradients, and layers in 4-bit blocks.
  *
  * All of them are asynchronous on hip_stream and return ZC_OK, ZC_ERR_ARG (nothing is launched then) or ZC_ERR_HIP; there is
- * nothing to finish.  They can be captured into a HIP graph.  Buffers need the alignment of their own type only, unless said
+ * nothing to finish.  They can be captured into a HIP graph (which keeps a step's number and factors as they were then).  Buffers need the alignment of their own type only, unless said
  * otherwise.  Sizes of zero are fine. */
 #define ZC_F32 0
 #define ZC_BF16 1
@@ -328,7 +328,7 @@ int zc_quality(const float* d_ref, const float* d_test, size_t n, double* out4,
  * A code is e4m3, a scale byte s stands for 2^(s - 127), 255 for a block with a value that is not finite (all NaN).  s is the exponent field
  * of the block's largest magnitude minus 7, at least 0.  Codes are rounded to the nearest (ties to even) if seed is 0, otherwise up or
  * down at random in proportion, which keeps small changes alive on average: value j of the state goes up when its 16 random bits
- * over 65536 reach the way that is left.  The bits are hashed from seed, step and j, so that equal calls give equal results.
+ * over 65536 reach the way that is left.  The bits are hashed from seed, step and j (of these two the low 32 bits), so that equal calls give equal results.
  * A root that is not zero never gets the code of zero.
  * step counts from 1.  Errors: ARG (also betas outside [0, 1), negative or not finite lr, eps, weight_decay, step 0, state too small), HIP. */
 size_t zc_adamw_state_bytes(const size_t* n, int k, int state_bits);
@@ -357,8 +357,9 @@ int zc_mx_dequantize(const void* d_codes, size_t codes_stride, const void* d_sca
 
 /* d_out (m x n, out_type, rows out_stride values apart) = the products of the rows of a (m x k) and of b (n x k), both held in blocks
  * along k, + d_bias (n binary32 values, may be NULL), + what is in d_out (flag ZC_MX_ADD).  Sums in binary32, rounded once.
- * The order of a sum depends on the sizes only, so that equal calls give equal results.
- * d_ws: zc_mx_workspace_bytes(m, n, k) bytes, 16-byte aligned; its content is irrelevant, and calls that may overlap need one each. */
+ * The order of a sum depends on the sizes only, so that equal calls give equal results.  m x n is at most 2^31 tiles of 64 x 64.
+ * d_ws: 16-byte aligned.  zc_mx_linear takes zc_mx_workspace_bytes(m, n, k) bytes, for its input in blocks (n does not matter to their number); the content is irrelevant, and calls
+ * that may overlap need one each.  zc_mx_product works without: any d_ws, NULL too. */
 #define ZC_MX_ADD 1u
 size_t zc_mx_workspace_bytes(size_t m, size_t n, size_t k);
 int zc_mx_product(const void* d_a, size_t a_stride, const void* d_a_scales, size_t a_scales_stride, const void* d_b, size_t b_stride,

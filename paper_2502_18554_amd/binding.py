@@ -556,7 +556,7 @@ def _product_end(d_w_codes, d_w_scales, k, d_out, d_bias):
 
 
 def zc_mx_product(d_a_codes, d_a_scales, d_b_codes, d_b_scales, k, d_out, d_ws, d_bias=None, add=False, stream=None):
-    """d_out (m x n) = a (m rows of k values, in blocks) times b (n rows) transposed, + d_bias, + d_out itself with add.  Returns the status."""
+    """d_out (m x n) = a (m rows of k values, in blocks) times b (n rows) transposed, + d_bias, + d_out itself with add; d_ws may be None.  Returns the status."""
     lib()
     if _native_layers:
         r = _native_layers.product(d_a_codes, d_a_scales, d_b_codes, d_b_scales, k, d_out, d_ws, d_bias, add, stream)

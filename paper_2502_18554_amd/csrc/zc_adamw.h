@@ -11,10 +11,11 @@
 // moves, which with b2 = 0.999 is nearly always.  So rounding is by default up or down with the probability that keeps the
 // mean, from 16 hashed bits per value and state (seed, step, place in the state).
 //
-// States in 32 bits: bound by memory (50 M values of 32 bits, gradients and copies of 16, 270 us, 5.2 TB/s, what a copy reaches; 4 groups of four values a lane, all of
-// whose loads are on their way before the first is used).  In 8 bits with weights of 32 bits as well (67 M values 205 us, 5.3 TB/s), with weights of 16 bits by arithmetic (9 M
-// values 24.9 us, 3.7 TB/s, 85 % of the vector instructions' issue time).  The tensors' table travels in the kernel's arguments, so that a step of 110 tensors is one launch that
-// nothing has to be copied for: 8 small tensors 2.3 us.
+// States in 32 bits: bound by memory (50 M values of 32 bits, gradients and copies of 16, 273 us, 5.1 TB/s, what a copy reaches; 4 groups of four values a lane, all of
+// whose loads are on their way before the first is used; 9 M values of 16 bits with gradients likewise 30.4 us, 6.5 TB/s, partly from the last cache).  In 8 bits with weights of 32 bits as
+// well (67 M values 205 us, 5.3 TB/s), with weights of 16 bits by arithmetic (9 M values 24.8 us, 3.7 TB/s, 92 vector instructions a value, 85 % of their issue time; the kind of rounding is
+// asked for at every value, and the hash's place costs a multiplication that an addition could be).  The tensors' table travels in the kernel's arguments, so that a step of
+// 110 tensors is one launch that nothing has to be copied for: 24 tensors of 1000 values 2.5 us.
 #pragma once
 
 #include "zc_values.h"
@@ -53,7 +54,8 @@ struct AdamwArgs {
 };
 static_assert(sizeof(AdamwArgs) <= 4096);
 
-// Scrambles a word (odd multipliers from the fractional parts of sqrt 2 and sqrt 3, folded by shifts).
+// Scrambles a word: the method of xxHash32's last mixing (Y. Collet: shifts by 15, 13 and 16 with a multiplication behind the first two), with other odd multipliers, the
+// fractional parts of sqrt 2 and sqrt 3.  Places are spread by that hash's first prime, 0x9E3779B1, next to 2^32 over the golden ratio (multiplicative hashing, Knuth).
 __host__ __device__ inline u32 mixed_word(u32 z) {
   z ^= z >> 15;
   z *= 0x6A09E667u;

@@ -100,8 +100,9 @@ struct MxQuantizeArgs {
 // 16384 x 16384 123 for 119).
 // Tiles follow each other along the rows in the order of the workgroups: neighbours are read at the same time.  (Runs of tiles for each XCD, along the rows or down the
 // columns, were slower by 5 to 20 %.)
-// Bound by memory: 8192 x 8192 in 16 bits along the rows 30 us (170 MB, 5.6 TB/s), along both axes 50 us (205 MB, 4.1 TB/s; tiles of 256 rows, which
-// write whole lines of codes down the columns too, took as long, and small matrices 20 % longer); 24 x 4096 2.3 us, a launch.
+// Bound by memory: 8192 x 8192 in 16 bits, again and again on inputs that no cache holds, along the rows 30 us (170 MB, 5.6 TB/s), along both axes 50 us (205 MB, 4.1 TB/s), on an
+// input in the last cache 26 and 39; right behind kernels that wrote as much or more, 38 to 45 and 68.  Down the columns a lane writes 16 bytes and a byte of lines of its own: of both axes
+// 100 MB are written for 71 (tiles of 256 rows, which write whole lines of codes there too, took as long, and small matrices 20 % longer); 24 x 4096 2.3 us, a launch.
 __host__ __device__ constexpr u32 mx_tile_bytes(bool down) { return down ? 256 : 1024; }
 __host__ __device__ constexpr u32 mx_quantize_rows(bool down) { return 32768 / mx_tile_bytes(down); }
 __host__ __device__ constexpr u32 mx_quantize_cols(int type, bool down) { return mx_tile_bytes(down) / (type == ZC_F32 ? 4 : 2); }
@@ -264,7 +265,7 @@ struct MxDequantizeArgs {
 
 // Four bytes of codes a thread and step: eight values, so that a wave's stores follow each other.  Pieces of eight are counted through the rows, `across` of them a
 // row; a quotient by it is a product with `inverse` (2^32 / across rounded up), one too large at most.  A thread asks for all of its pieces before it writes the first.  Bound by
-// what it writes: 8192 x 8192 to 16 bits 25.6 us (6.6 TB/s, partly from the last cache), to 32 bits 60 us (5.1 TB/s); 77 x 1001 2.0 us, a launch.
+// what it writes: 8192 x 8192 to 16 bits 25.8 us (6.6 TB/s, partly from the last cache), to 32 bits 60 us (5.1 TB/s); 77 x 1001 2.0 us, a launch.
 template <int TYPE, u32 PIECES>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(MxDequantizeArgs a, u32 across, u32 inverse, u32 pieces) {
   using One = typename ValueOf<TYPE>::One;

@@ -1,11 +1,13 @@
 // Products of few rows (up to 32) with many: serving, a token or some at a time.  What bounds them is reading b once.
 //
 // A workgroup makes all rows' results of 16 CG columns; its waves take turns along k, by spans of 16 blocks, and add up in LDS in the end, wave by wave, so that
-// a sum's order depends on the sizes only.  A wave reads four blocks (64 bytes) of 16 rows of b with one load, and keeps the loads of a span in flight.
-// Rows of a come as they are held, or (up to 8) as values: then a lane quantises the block that it brings to the instruction, in registers: some 60 operations for
-// every four loads, mostly hidden behind them, where a launch of its own for that takes half as long as the product.
-// 1 row x 4096 x 4096 4.3 us, held 3.3 (9 MB at 2.7 TB/s; some 2 of it are a launch's, the rest two rounds of loads, for the scales and codes of a span, and the sum over the waves);
-// 24 held rows x 16384 x 4096 10.8 us (36 MB at 3.4 TB/s).
+// a sum's order depends on the sizes only.  A wave reads four blocks (64 bytes) of 16 rows of b with one load.
+// Rows of a come as they are held, or (up to 8) as values: then a lane quantises the block that it brings to the instruction, in registers, some 60 operations a block,
+// where a launch of its own for that takes half as long as the product.
+// Bound by loads that wait for each other, more than by their bytes.  The source asks for all loads of a span ahead of the first use; compiled, they come in rounds, in 60 registers of the
+// 256 that a lane could have: of a row of 16-bit values the four steps one after the other, each loaded, waited for and quantised, then the scales and two loads of b, then the other two: seven
+// rounds a span; of 32 held rows by 64 columns, in 120 registers, seven waits for all that is on its way.
+// 1 row x 4096 x 4096 4.3 us, held 3.3 (9 MB at 2.7 TB/s; some 2 of it are a launch's); 24 held rows x 16384 x 4096 10.9 us (36 MB at 3.4 TB/s).
 #pragma once
 
 #include "zc_mx_product.h"
@@ -103,7 +105,7 @@ __device__ inline u32x4_t mx_span_scales(const u8* row, u32 first, u32 blocks) {
 // WHOLE: rows are whole spans, and every wave takes them as such: no step, block or value is missing anywhere.
 template <int RG, int CG, int X, bool WHOLE>
 __global__ __launch_bounds__(64 * kFewWaves) void mx_few_kernel(MxFewArgs a) {
-  // Steps whose values of a are on their way together: as many as leave room for b's.
+  // Steps whose values of a are asked for together: as many as leave room for b's.
   constexpr u32 AHEAD = X == kHeldRows ? 4 : 64 / (RG * (X == ZC_F32 ? 32 : 16));
   constexpr bool SPANS = WHOLE || X == kHeldRows;       // a wave takes whole spans
   __shared__ f32x4_t parts[kFewWaves * RG * CG * 64];

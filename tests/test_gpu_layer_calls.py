@@ -128,3 +128,12 @@ def test_both_ways_are_alike(monkeypatch, kind):
     monkeypatch.setattr(b, "_native_layers", None)
     other = results(kind)
     assert len(one) == len(other) and all(torch.equal(s, t) for s, t in zip(one, other))
+
+
+@pytest.mark.parametrize("m", [4, 40])
+def test_products_need_no_workspace(way, m):
+    n, k = 48, 200
+    a, w, one, other = room(m, k, 0x22), room(n, k, 0x31), torch.empty(m, n, device=DEV), torch.empty(m, n, device=DEV)
+    assert zc.zc_mx_product(*a, *w, k, one, torch.empty(zc.zc_mx_workspace_bytes(m, n, k), dtype=torch.uint8, device=DEV)) == ZC_OK
+    assert zc.zc_mx_product(*a, *w, k, other, None) == ZC_OK
+    assert torch.equal(one, other)
