@@ -372,6 +372,61 @@ int zc_mx_linear(const void* d_x, int x_type, size_t x_stride, const void* d_w, 
                  size_t m, size_t n, size_t k, const float* d_bias, void* d_out, int out_type, size_t out_stride, unsigned flags, void* d_ws,
                  size_t ws_bytes, void* hip_stream);
 
+/* Flags of the calls below: a result is added to what its buffer holds. */
+#define ZC_ADD 1u
+#define ZC_ADD_WEIGHTS 2u
+
+/* Layer norm of the rows of d_x (rows x cols values of x_type, rows x_stride values apart), in binary32:
+ *   mean = sum x / cols;  d = 1 / sqrt(sum (x - mean)^2 / cols + eps);  out = (x - mean) d w + b
+ * rounded once, to out_type.  d_w, d_b: cols values of w_type each, either may be NULL (1 and 0).  d_stats (may be NULL): 2 rows binary32 values, the
+ * rows' means, then their d, for the backward pass.  d_out may be d_x, of the same type and stride.
+ * A row with a value that is not finite becomes NaNs.  rows below 2^31, cols up to 2^27.  Errors: ARG, HIP. */
+int zc_layer_norm(const void* d_x, int x_type, size_t rows, size_t cols, size_t x_stride, const void* d_w, const void* d_b, int w_type, double eps,
+                  void* d_out, int out_type, size_t out_stride, float* d_stats, void* hip_stream);
+
+/* Its gradients, from that of its output, d_dy.  With z = (x - mean) d and h = dy w:
+ *   dx = d (h - sum h / cols - z sum (h z) / cols);  dw = sum over the rows of dy z;  db = sum over the rows of dy
+ * d_dx, d_dw, d_db: any may be NULL.  ZC_ADD: dx is added to what d_dx holds (the gradient of a residual stream); ZC_ADD_WEIGHTS: dw and db
+ * likewise.  d_dx may be d_dy or d_x, of the same type and stride.  Sums in binary32, results rounded once; their order depends on the sizes only, so that
+ * equal calls give equal results.  No rows: dw and db are zeros.  d_ws: 16-byte aligned, its content irrelevant, one for calls that may overlap. */
+size_t zc_layer_norm_workspace_bytes(size_t rows, size_t cols);
+int zc_layer_norm_backward(const void* d_dy, int dy_type, size_t dy_stride, const void* d_x, int x_type, size_t x_stride, const float* d_stats, const void* d_w,
+                           int w_type, size_t rows, size_t cols, void* d_dx, int dx_type, size_t dx_stride, void* d_dw, void* d_db, int dw_type, unsigned flags,
+                           void* d_ws, size_t ws_bytes, void* hip_stream);
+
+/* Rows of a table by tokens: out[i] = scale x table[token[i]], rounded once; zeros where token[i] is not in [0, table_rows), as padding is.  d_tokens: n whole numbers with sign, of
+ * token_bits 32 or 64.  Up to 2^29 rows of up to 2^23 values; n below 2^31.  Errors: ARG, HIP. */
+int zc_embedding(const void* d_table, int table_type, size_t table_rows, size_t cols, size_t table_stride, const void* d_tokens, int token_bits, size_t n, double scale,
+                 void* d_out, int out_type, size_t out_stride, void* hip_stream);
+
+/* The table's gradient from that of the output, d_dy (n x cols): grad[v] = scale x the sum of dy[i] over all i with token[i] = v, zeros for a row that no token
+ * names.  ZC_ADD: added to what d_grad holds; rows that no token names stay as they are.  Sums in binary32, rounded once; their order depends on the sizes and
+ * the tokens only, so that equal calls give equal results.  d_ws: 16-byte aligned, its content irrelevant, one for calls that may overlap. */
+size_t zc_embedding_workspace_bytes(size_t n, size_t table_rows, size_t cols);
+int zc_embedding_backward(const void* d_dy, int dy_type, size_t dy_stride, const void* d_tokens, int token_bits, size_t n, double scale, void* d_grad, int grad_type,
+                          size_t table_rows, size_t cols, size_t grad_stride, unsigned flags, void* d_ws, size_t ws_bytes, void* hip_stream);
+
+/* One optimiser step over k matrices (rows[i] x cols[i] values in one piece; host arrays of k entries) whose momentum is made nearly orthogonal (Jordan et al., "Muon", 2024).
+ * In binary32, with X the matrix, turned where it has more rows than columns:
+ *   g = grad x *d_grad_scale;  m' = momentum m + (1 - momentum) g;  u = momentum m' + (1 - momentum) g with ZC_MUON_NESTEROV, m' without
+ *   X = u / max(root of the sum of u^2, 1e-7);  `iterations` times:  A = X X^T,  B = -4.7750 A + 2.0315 A A,  X = 3.4445 X + B X
+ *   p' = p (1 - lr weight_decay) - lr factor X
+ * factor: sqrt(max(1, rows / cols)); with ZC_MUON_MATCH_RMS 0.2 sqrt(max(rows, cols)).
+ * The products' operands are X, A and B rounded to 11 bits (binary16, scaled by 2^12), with ZC_MUON_WIDE to 22 bits (two of them; three times the work), sums are in
+ * binary32: p' is off by at most some 2^-9, 2^-18 with ZC_MUON_WIDE, of lr factor times a typical value of X.
+ * param_type, grad_type, d_copies, copy_type, d_grad_scale: as in zc_adamw (a scale that is not finite: nothing changes).  A gradient with a value that is not finite makes its
+ * matrix's p' and what it touches of m' NaNs.  d_state: zc_muon_state_bytes bytes, 16-byte aligned, zeros before the first step: m of all matrices in their order as binary32 values, each
+ * filled up to a multiple of 32 of them.  d_ws: zc_muon_workspace_bytes bytes, 256-byte aligned, its content irrelevant, one for calls that may overlap.  Equal calls
+ * give equal results.  Up to 2^20 rows and columns, 1 to 100 iterations.  Errors: ARG, HIP. */
+#define ZC_MUON_NESTEROV 1u
+#define ZC_MUON_MATCH_RMS 2u
+#define ZC_MUON_WIDE 4u
+size_t zc_muon_state_bytes(int k, const size_t* rows, const size_t* cols);
+size_t zc_muon_workspace_bytes(int k, const size_t* rows, const size_t* cols, unsigned flags);
+int zc_muon(int k, const size_t* rows, const size_t* cols, void* const* d_params, int param_type, const void* const* d_grads, int grad_type,
+            void* const* d_copies, int copy_type, void* d_state, size_t state_bytes, double lr, double momentum, double weight_decay, int iterations, unsigned flags,
+            const float* d_grad_scale, void* d_ws, size_t ws_bytes, void* hip_stream);
+
 /* Completes an asynchronous call: synchronises hip_stream, returns the status of the last
  * call that used d_ws and stores its size result (total_bytes, or n for zc_decompress) in
  * *result (host, may be NULL).  d_ws NULL: the call was zc_compress_noalloc on the current device. */

@@ -29,6 +29,8 @@ EXPORTS = [
     "zc_profile_enable", "zc_profile_collect",
     "zc_adamw", "zc_adamw_state_bytes", "zc_mx_codes_stride", "zc_mx_scales_stride", "zc_mx_quantize", "zc_mx_dequantize", "zc_mx_workspace_bytes",
     "zc_mx_product", "zc_mx_linear",
+    "zc_layer_norm", "zc_layer_norm_workspace_bytes", "zc_layer_norm_backward", "zc_embedding", "zc_embedding_workspace_bytes", "zc_embedding_backward",
+    "zc_muon", "zc_muon_state_bytes", "zc_muon_workspace_bytes",
 ]
 
 _lib = None
@@ -93,6 +95,17 @@ def lib():
         L.zc_mx_dequantize.argtypes = [vp, sz, vp, sz, sz, sz, vp, i, sz, vp]
         L.zc_mx_product.argtypes = [vp, sz, vp, sz, vp, sz, vp, sz, sz, sz, sz, vp, vp, i, sz, u, vp, sz, vp]
         L.zc_mx_linear.argtypes = [vp, i, sz, vp, sz, vp, sz, sz, sz, sz, vp, vp, i, sz, u, vp, sz, vp]
+        for name in ("zc_layer_norm_workspace_bytes", "zc_embedding_workspace_bytes", "zc_muon_state_bytes", "zc_muon_workspace_bytes"):
+            getattr(L, name).restype = sz
+        L.zc_layer_norm_workspace_bytes.argtypes = [sz, sz]
+        L.zc_layer_norm.argtypes = [vp, i, sz, sz, sz, vp, vp, i, d, vp, i, sz, vp, vp]
+        L.zc_layer_norm_backward.argtypes = [vp, i, sz, vp, i, sz, vp, vp, i, sz, sz, vp, i, sz, vp, vp, i, u, vp, sz, vp]
+        L.zc_embedding_workspace_bytes.argtypes = [sz, sz, sz]
+        L.zc_embedding.argtypes = [vp, i, sz, sz, sz, vp, i, sz, d, vp, i, sz, vp]
+        L.zc_embedding_backward.argtypes = [vp, i, sz, vp, i, sz, d, vp, i, sz, sz, sz, u, vp, sz, vp]
+        L.zc_muon_state_bytes.argtypes = [i, vp, vp]
+        L.zc_muon_workspace_bytes.argtypes = [i, vp, vp, u]
+        L.zc_muon.argtypes = [i, vp, vp, vp, i, vp, i, vp, i, vp, sz, d, d, d, i, u, vp, vp, sz, vp]
         L.zc_profile_enable.argtypes = [C.c_int]
         L.zc_profile_collect.argtypes = [C.POINTER(C.c_float), C.POINTER(C.c_int), C.c_int]
         _lib = L
@@ -132,6 +145,7 @@ def _load_native(L):
     calls = (L.zc_adamw, L.zc_mx_quantize, L.zc_mx_dequantize, L.zc_mx_product, L.zc_mx_linear)
     if layers.setup_layers(*(C.cast(f, C.c_void_p).value for f in calls), str(torch.__version__).split("+")[0]):
         _native_layers = layers
+        layers.setup_training(*(C.cast(f, C.c_void_p).value for f in (L.zc_layer_norm, L.zc_layer_norm_backward, L.zc_embedding, L.zc_embedding_backward, L.zc_muon)))
 
 
 # Small calls are bound by what happens here (a chunk of a few thousand values runs for 4 us).  Where ctypes takes a call, addresses go to
@@ -587,3 +601,153 @@ def zc_mx_linear(d_x, d_w_codes, d_w_scales, d_out, d_ws, d_bias=None, add=False
     out, w = end
     return lib().zc_mx_linear(x[0], x[1], x[4], *w, out[2], out[3], x[3], _p(d_bias), out[0], out[1], out[4], ZC_MX_ADD if add else 0, _p(d_ws),
                               _size(d_ws) if d_ws is not None else 0, _stream(stream))
+
+
+# ---- The other calls of a training step.  Tensors are on torch's current device, whose current stream a call without one goes to.
+
+ZC_ADD, ZC_ADD_WEIGHTS = 1, 2
+ZC_MUON_NESTEROV, ZC_MUON_MATCH_RMS, ZC_MUON_WIDE = 1, 2, 4
+_TOKENS = {torch.int32: 32, torch.int64: 64}
+
+
+def _here(*tensors):
+    """Whether all of these that are there are on the current device."""
+    there = [t for t in tensors if t is not None]
+    return all(t.is_cuda for t in there) and (not there or {t.device.index for t in there} == {torch._C._cuda_getDevice()})
+
+
+def _vectors(n, *tensors):
+    """(type, addresses) of tensors, or None for each, of n values in one piece and of one type; None for others."""
+    there = [t for t in tensors if t is not None]
+    if not all(t.is_cuda and t.is_contiguous() and t.numel() == n for t in there) or (there and _one_type(there) < 0):
+        return None
+    return (_one_type(there), *(_p(t) for t in tensors))
+
+
+def _alike(a, b):
+    return a is not None and b is not None and a[2:4] == b[2:4]
+
+
+def zc_layer_norm_workspace_bytes(rows, cols):
+    return int(lib().zc_layer_norm_workspace_bytes(int(rows), int(cols)))
+
+
+def zc_layer_norm(d_x, d_w, d_b, d_out, d_stats=None, eps=1e-5, stream=None):
+    """d_out = the layer norm of the rows of d_x, with weights and bias (contiguous, of one type, either may be None); d_stats: 2 x rows binary32 values
+    for the backward pass, or None.  d_out may be d_x.  Returns the status."""
+    lib()
+    if _native_layers:
+        r = _native_layers.layer_norm(d_x, d_w, d_b, d_out, d_stats, eps, stream)
+        if r is not NotImplemented:
+            return r
+    x, out = _matrix(d_x), _matrix(d_out)
+    if not _alike(x, out) or not _here(d_x, d_w, d_b, d_out, d_stats):
+        return ZC_ERR_ARG
+    weights, stats = _vectors(x[3], d_w, d_b), _vectors(2 * x[2], d_stats)
+    if weights is None or stats is None or stats[0] != ZC_F32:
+        return ZC_ERR_ARG
+    return lib().zc_layer_norm(*x, weights[1], weights[2], weights[0], float(eps), out[0], out[1], out[4], stats[1], _stream(stream))
+
+
+def zc_layer_norm_backward(d_dy, d_x, d_stats, d_w, d_dx, d_dw, d_db, d_ws, add=False, add_weights=False, stream=None):
+    """The gradients of zc_layer_norm's input, weights and bias (d_dx, d_dw, d_db: any may be None) from that of its output; add: d_dx is added to, add_weights: d_dw and
+    d_db are.  Returns the status."""
+    lib()
+    if _native_layers:
+        r = _native_layers.layer_norm_backward(d_dy, d_x, d_stats, d_w, d_dx, d_dw, d_db, d_ws, add, add_weights, stream)
+        if r is not NotImplemented:
+            return r
+    dy, x, dx = _matrix(d_dy), _matrix(d_x), _matrix(d_dx) if d_dx is not None else None
+    if not _alike(dy, x) or (d_dx is not None and not _alike(dx, x)) or d_stats is None or not _here(d_dy, d_x, d_stats, d_w, d_dx, d_dw, d_db, d_ws) or not _own_bytes(d_ws):
+        return ZC_ERR_ARG
+    weights, stats, sums = _vectors(x[3], d_w), _vectors(2 * x[2], d_stats), _vectors(x[3], d_dw, d_db)
+    if weights is None or stats is None or sums is None or stats[0] != ZC_F32:
+        return ZC_ERR_ARG
+    return lib().zc_layer_norm_backward(dy[0], dy[1], dy[4], x[0], x[1], x[4], stats[1], weights[1], weights[0], x[2], x[3], *((dx[0], dx[1], dx[4]) if dx else (None, ZC_F32, 0)),
+                                        sums[1], sums[2], sums[0], (ZC_ADD if add else 0) | (ZC_ADD_WEIGHTS if add_weights else 0), _p(d_ws),
+                                        _size(d_ws) if d_ws is not None else 0, _stream(stream))
+
+
+def _tokens(t, rows):
+    """(address, bits) of as many tokens as there are rows, or None."""
+    if t.dtype not in _TOKENS or not t.is_cuda or not t.is_contiguous() or t.numel() != rows:
+        return None
+    return t.data_ptr(), _TOKENS[t.dtype]
+
+
+def zc_embedding(d_table, d_tokens, d_out, scale=1.0, stream=None):
+    """d_out (a row for each token) = scale times the tokens' rows of d_table, zeros for tokens outside it.  d_tokens: int32 or int64, of any shape, contiguous.  Returns the status."""
+    lib()
+    if _native_layers:
+        r = _native_layers.embedding(d_table, d_tokens, d_out, scale, stream)
+        if r is not NotImplemented:
+            return r
+    table, out = _matrix(d_table), _matrix(d_out)
+    tokens = out and _tokens(d_tokens, out[2])
+    if not table or not tokens or table[3] != out[3] or not _here(d_table, d_tokens, d_out):
+        return ZC_ERR_ARG
+    return lib().zc_embedding(*table, *tokens, out[2], float(scale), out[0], out[1], out[4], _stream(stream))
+
+
+def zc_embedding_workspace_bytes(n, table_rows, cols):
+    return int(lib().zc_embedding_workspace_bytes(int(n), int(table_rows), int(cols)))
+
+
+def zc_embedding_backward(d_dy, d_tokens, d_grad, d_ws, scale=1.0, add=False, stream=None):
+    """d_grad (a row for each of the table's) = scale times the sums of the rows of d_dy by token, or that added to what it holds.  Returns the status."""
+    lib()
+    if _native_layers:
+        r = _native_layers.embedding_backward(d_dy, d_tokens, d_grad, d_ws, scale, add, stream)
+        if r is not NotImplemented:
+            return r
+    dy, grad = _matrix(d_dy), _matrix(d_grad)
+    tokens = dy and _tokens(d_tokens, dy[2])
+    if not grad or not tokens or dy[3] != grad[3] or not _here(d_dy, d_tokens, d_grad, d_ws) or not _own_bytes(d_ws):
+        return ZC_ERR_ARG
+    return lib().zc_embedding_backward(dy[0], dy[1], dy[4], *tokens, dy[2], float(scale), grad[0], grad[1], grad[2], grad[3], grad[4], ZC_ADD if add else 0, _p(d_ws),
+                                       _size(d_ws) if d_ws is not None else 0, _stream(stream))
+
+
+def _shapes(shapes):
+    rows, cols = _words([int(r) for r, _ in shapes]), _words([int(c) for _, c in shapes])
+    return len(shapes), rows, cols
+
+
+def zc_muon_state_bytes(shapes):
+    """Bytes of the state of matrices with these (rows, columns); 0 for what there is no state of."""
+    k, rows, cols = _shapes(shapes)
+    return int(lib().zc_muon_state_bytes(k, rows[1], cols[1]))
+
+
+def zc_muon_workspace_bytes(shapes, wide=False):
+    k, rows, cols = _shapes(shapes)
+    return int(lib().zc_muon_workspace_bytes(k, rows[1], cols[1], ZC_MUON_WIDE if wide else 0))
+
+
+def zc_muon(d_params, d_grads, d_state, d_ws, lr, momentum=0.95, weight_decay=0.0, iterations=5, nesterov=True, match_rms=False, wide=False, d_copies=None, d_grad_scale=None,
+            stream=None):
+    """One step with orthogonalised momentum over the matrices of the list d_params (contiguous, of one type; d_grads: as many of the same shapes, of one type), in
+    place.  d_copies: None, or a list with a matrix or None for each.  Returns the status."""
+    lib()
+    flags = (ZC_MUON_NESTEROV if nesterov else 0) | (ZC_MUON_MATCH_RMS if match_rms else 0) | (ZC_MUON_WIDE if wide else 0)
+    if _native_layers:
+        r = _native_layers.muon(d_params, d_grads, d_state, d_ws, lr, momentum, weight_decay, iterations, flags, d_copies, d_grad_scale, stream)
+        if r is not NotImplemented:
+            return r
+    k = len(d_params)
+    if len(d_grads) != k or (d_copies is not None and len(d_copies) != k):
+        return ZC_ERR_ARG
+    copies = [] if d_copies is None else [t for t in d_copies if t is not None]
+    shapes = [tuple(t.shape) for t in d_params]
+    if any(len(s) != 2 for s in shapes) or [tuple(t.shape) for t in d_grads] != shapes or not all(t.is_contiguous() for t in (*d_params, *d_grads, *copies)) or \
+            any(t is not None and tuple(t.shape) != s for t, s in zip(d_copies or (), shapes)) or not _here(*d_params, *d_grads, *copies, d_state, d_ws, d_grad_scale) or \
+            not _own_bytes(d_state) or not _own_bytes(d_ws) or (d_grad_scale is not None and (d_grad_scale.dtype != torch.float32 or d_grad_scale.numel() != 1)):
+        return ZC_ERR_ARG
+    _, rows, cols = _shapes(shapes)
+    lists = [_words([t.data_ptr() for t in d_params]), _words([t.data_ptr() for t in d_grads]),
+             _words([t.data_ptr() if t is not None else 0 for t in d_copies]) if d_copies is not None else (None, None)]
+    if not 0 <= int(iterations) < 1 << 31:
+        return ZC_ERR_ARG
+    return lib().zc_muon(k, rows[1], cols[1], lists[0][1], _one_type(d_params), lists[1][1], _one_type(d_grads), lists[2][1], _one_type(copies), _p(d_state),
+                         _size(d_state) if d_state is not None else 0, float(lr), float(momentum), float(weight_decay), int(iterations), flags, _p(d_grad_scale), _p(d_ws),
+                         _size(d_ws) if d_ws is not None else 0, _stream(stream))

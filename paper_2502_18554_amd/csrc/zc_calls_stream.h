@@ -30,6 +30,17 @@ struct Streams {
     Py_DECREF(now);
     return handle(r, stream);
   }
+  // Torch's current device, -1 where there is none of a plain form.
+  int current() const {
+    PyObject* const now = device ? PyObject_CallNoArgs(device) : nullptr;
+    const long v = now && PyLong_CheckExact(now) ? PyLong_AsLong(now) : -1;
+    Py_XDECREF(now);
+    if (PyErr_Occurred()) {
+      PyErr_Clear();
+      return -1;
+    }
+    return int(v);
+  }
   static bool handle(PyObject* r, void*& stream) {
     if (!r) return false;
     uint64_t v = 0;

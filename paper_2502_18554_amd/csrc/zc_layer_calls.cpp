@@ -1,4 +1,4 @@
-// The calls around the collective (zc_adamw, zc_mx_*) in native code: from torch's tensors to the C ABI of libzc.so.
+// The calls around the collective (zc_adamw, zc_mx_*, zc_layer_norm, zc_embedding, zc_muon) in native code: from torch's tensors to the C ABI of libzc.so.
 //
 // A step over a list of tensors asks each of them for address, size, type and layout.  From Python, or through Python's attributes, that is 0.4 to 0.8 us a
 // tensor, more than the step itself takes on small ones; here the tensors are read as what they are, 20 ns each.  That needs the headers
@@ -28,6 +28,11 @@ struct Calls {
   decltype(&zc_mx_dequantize) dequantize;
   decltype(&zc_mx_product) product;
   decltype(&zc_mx_linear) linear;
+  decltype(&zc_layer_norm) layer_norm;
+  decltype(&zc_layer_norm_backward) layer_norm_backward;
+  decltype(&zc_embedding) embedding;
+  decltype(&zc_embedding_backward) embedding_backward;
+  decltype(&zc_muon) muon;
 } g_calls;
 
 PyObject* not_this_way() {
@@ -231,6 +236,168 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return answer(st);
 }
 
+// Whether all of these that are tensors are on torch's current device.
+bool on_current_device(PyObject* const* a, Py_ssize_t n) {
+  const int now = g_streams.current();
+  for (Py_ssize_t i = 0; i < n; ++i)
+    if (THPVariable_CheckExact(a[i]) && (!tensor(a[i]) || THPVariable_Unpack(a[i]).device().index() != now)) return false;
+  return now >= 0;
+}
+// n values of one of the three types in one piece, or None.
+bool values_of(PyObject* o, size_t n, void*& p, int& type, bool& there) {
+  p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* const t = tensor(o);
+  if (!t || !t->is_contiguous() || size_t(t->numel()) != n) return false;
+  const int kind = type_of(*t);
+  if (kind < 0 || (there && kind != type)) return false;
+  type = kind;
+  there = true;
+  p = t->data_ptr();
+  return true;
+}
+bool stats_of(PyObject* o, size_t rows, float*& p) {
+  void* at;
+  int type = ZC_F32;
+  bool there = false;
+  if (!values_of(o, 2 * rows, at, type, there) || type != ZC_F32) return false;
+  p = static_cast<float*>(at);
+  return true;
+}
+bool tokens_of(PyObject* o, size_t rows, const void*& p, int& bits) {
+  const at::Tensor* const t = tensor(o);
+  if (!t || !t->is_contiguous() || size_t(t->numel()) != rows) return false;
+  bits = t->scalar_type() == at::kLong ? 64 : t->scalar_type() == at::kInt ? 32 : 0;
+  p = t->data_ptr();
+  return bits != 0;
+}
+bool truth(PyObject* o, bool& v) {
+  if (!PyBool_Check(o)) return false;
+  v = o == Py_True;
+  return true;
+}
+
+// (d_x, d_w, d_b, d_out, d_stats, eps, stream)
+PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  Matrix x, out;
+  void *w, *b, *stream;
+  float* stats;
+  int w_type = ZC_F32;
+  bool there = false;
+  double eps;
+  if (n_args != 7 || !on_current_device(a, 5) || !matrix(a[0], x) || !matrix(a[3], out) || out.rows != x.rows || out.cols != x.cols || !values_of(a[1], x.cols, w, w_type, there) ||
+      !values_of(a[2], x.cols, b, w_type, there) || !stats_of(a[4], x.rows, stats) || !real(a[5], eps) || !stream_of(a[6], stream))
+    return not_this_way();
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = g_calls.layer_norm(x.at, x.type, x.rows, x.cols, x.stride, w, b, w_type, eps, out.at, out.type, out.stride, stats, stream);
+  Py_END_ALLOW_THREADS
+  return answer(st);
+}
+
+// (d_dy, d_x, d_stats, d_w, d_dx, d_dw, d_db, d_ws, add, add_weights, stream)
+PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  Matrix dy, x, dx{nullptr, ZC_F32, 0, 0, 0};
+  void *w, *dw, *db, *ws, *stream;
+  float* stats;
+  int w_type = ZC_F32, dw_type = ZC_F32;
+  bool there = false, there_too = false, add, add_weights;
+  size_t ws_bytes;
+  if (n_args != 11 || !on_current_device(a, 8) || !matrix(a[0], dy) || !matrix(a[1], x) || dy.rows != x.rows || dy.cols != x.cols || a[2] == Py_None || !stats_of(a[2], x.rows, stats) ||
+      !values_of(a[3], x.cols, w, w_type, there) || (a[4] != Py_None && (!matrix(a[4], dx) || dx.rows != x.rows || dx.cols != x.cols)) || !values_of(a[5], x.cols, dw, dw_type, there_too) ||
+      !values_of(a[6], x.cols, db, dw_type, there_too) || !workspace_of(a[7], ws, ws_bytes) || !truth(a[8], add) || !truth(a[9], add_weights) || !stream_of(a[10], stream))
+    return not_this_way();
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = g_calls.layer_norm_backward(dy.at, dy.type, dy.stride, x.at, x.type, x.stride, stats, w, w_type, x.rows, x.cols, dx.at, dx.type, dx.stride, dw, db, dw_type,
+                                   (add ? ZC_ADD : 0u) | (add_weights ? ZC_ADD_WEIGHTS : 0u), ws, ws_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return answer(st);
+}
+
+// (d_table, d_tokens, d_out, scale, stream)
+PyObject* embedding(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  Matrix table, out;
+  const void* tokens;
+  void* stream;
+  int bits;
+  double scale;
+  if (n_args != 5 || !on_current_device(a, 3) || !matrix(a[0], table) || !matrix(a[2], out) || table.cols != out.cols || !tokens_of(a[1], out.rows, tokens, bits) || !real(a[3], scale) ||
+      !stream_of(a[4], stream))
+    return not_this_way();
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = g_calls.embedding(table.at, table.type, table.rows, table.cols, table.stride, tokens, bits, out.rows, scale, out.at, out.type, out.stride, stream);
+  Py_END_ALLOW_THREADS
+  return answer(st);
+}
+
+// (d_dy, d_tokens, d_grad, d_ws, scale, add, stream)
+PyObject* embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  Matrix dy, grad;
+  const void* tokens;
+  void *ws, *stream;
+  int bits;
+  double scale;
+  bool add;
+  size_t ws_bytes;
+  if (n_args != 7 || !on_current_device(a, 4) || !matrix(a[0], dy) || !matrix(a[2], grad) || dy.cols != grad.cols || !tokens_of(a[1], dy.rows, tokens, bits) ||
+      !workspace_of(a[3], ws, ws_bytes) || !real(a[4], scale) || !truth(a[5], add) || !stream_of(a[6], stream))
+    return not_this_way();
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = g_calls.embedding_backward(dy.at, dy.type, dy.stride, tokens, bits, dy.rows, scale, grad.at, grad.type, grad.rows, grad.cols, grad.stride, add ? ZC_ADD : 0u, ws, ws_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return answer(st);
+}
+
+// A list's matrices, of one type and contiguous, on a device; sizes (rows, then columns) are written or, `same`, compared.
+bool matrices_of(PyObject* list, Py_ssize_t k, bool same, int device, std::vector<size_t>& sizes, void** to, int& type) {
+  if (!PyList_CheckExact(list) || PyList_GET_SIZE(list) != k) return false;
+  for (Py_ssize_t i = 0; i < k; ++i) {
+    const at::Tensor* const t = tensor(PyList_GET_ITEM(list, i));
+    if (!t || t->dim() != 2 || !t->is_contiguous() || t->device().index() != device) return false;
+    const int kind = type_of(*t);
+    if (kind < 0 || (i && kind != type)) return false;
+    type = kind;
+    const size_t rows = size_t(t->size(0)), cols = size_t(t->size(1));
+    if (same && (sizes[size_t(i)] != rows || sizes[size_t(k + i)] != cols)) return false;
+    sizes[size_t(i)] = rows, sizes[size_t(k + i)] = cols;
+    to[i] = t->data_ptr();
+  }
+  return true;
+}
+
+// (d_params, d_grads, d_state, d_ws, lr, momentum, weight_decay, iterations, flags, d_copies, d_grad_scale, stream)
+PyObject* muon(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  uint64_t iterations, flags;
+  double c[3];
+  void *state, *ws, *stream;
+  size_t state_bytes, ws_bytes;
+  const float* scale;
+  if (n_args != 12 || !PyList_CheckExact(a[0]) || !PyList_GET_SIZE(a[0])) return not_this_way();
+  const Py_ssize_t k = PyList_GET_SIZE(a[0]);
+  const int device = g_streams.current();
+  if (device < 0 || k > 0x7fffffff || !word(a[7], iterations) || iterations > 1000 || !word(a[8], flags) || flags > 0xffffffffu) return not_this_way();
+  for (int i = 0; i < 3; ++i)
+    if (!real(a[4 + i], c[i])) return not_this_way();
+  std::vector<size_t> sizes(static_cast<size_t>(2 * k));
+  std::vector<void*> at(static_cast<size_t>(3 * k));
+  int types[3] = {ZC_F32, ZC_F32, ZC_F32};
+  const bool copies = a[9] != Py_None;
+  PyObject* const others[3] = {a[2], a[3], a[10]};
+  if (!on_current_device(others, 3) || !matrices_of(a[0], k, false, device, sizes, at.data(), types[0]) || !matrices_of(a[1], k, true, device, sizes, at.data() + k, types[1]) ||
+      (copies && !matrices_of(a[9], k, true, device, sizes, at.data() + 2 * k, types[2])) || !workspace_of(a[2], state, state_bytes) || !workspace_of(a[3], ws, ws_bytes) ||
+      !bias_of(a[10], 1, scale) || !stream_of(a[11], stream))
+    return not_this_way();
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = g_calls.muon(int(k), sizes.data(), sizes.data() + k, at.data(), types[0], const_cast<const void* const*>(at.data() + k), types[1], copies ? at.data() + 2 * k : nullptr, types[2], state,
+                    state_bytes, c[0], c[1], c[2], int(iterations), unsigned(flags), scale, ws, ws_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return answer(st);
+}
+
 // (addresses of the five calls in the order of Calls, torch's version): whether the module can be used.
 PyObject* setup_layers(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   uint64_t at[5];
@@ -250,6 +417,26 @@ PyObject* setup_layers(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   g_calls.product = reinterpret_cast<decltype(g_calls.product)>(at[3]);
   g_calls.linear = reinterpret_cast<decltype(g_calls.linear)>(at[4]);
   Py_RETURN_TRUE;
+}
+
+// (addresses of the five calls behind those)
+PyObject* setup_training(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  uint64_t at[5];
+  if (n_args != 5) {
+    PyErr_SetString(PyExc_TypeError, "setup_training takes five addresses");
+    return nullptr;
+  }
+  for (int i = 0; i < 5; ++i)
+    if (!word(a[i], at[i]) || !at[i]) {
+      PyErr_SetString(PyExc_ValueError, "setup_training: the address of a call is missing");
+      return nullptr;
+    }
+  g_calls.layer_norm = reinterpret_cast<decltype(g_calls.layer_norm)>(at[0]);
+  g_calls.layer_norm_backward = reinterpret_cast<decltype(g_calls.layer_norm_backward)>(at[1]);
+  g_calls.embedding = reinterpret_cast<decltype(g_calls.embedding)>(at[2]);
+  g_calls.embedding_backward = reinterpret_cast<decltype(g_calls.embedding_backward)>(at[3]);
+  g_calls.muon = reinterpret_cast<decltype(g_calls.muon)>(at[4]);
+  Py_RETURN_NONE;
 }
 
 // (torch's current device, its raw current stream)
@@ -278,7 +465,9 @@ PyMethodDef method(const char* name) {
 }
 
 PyMethodDef g_methods[] = {method<setup_layers>("setup_layers"), method<setup_streams>("setup_streams"), method<adamw>("adamw"), method<quantize>("quantize"),
-                           method<dequantize>("dequantize"), method<product>("product"), method<linear>("linear"), {nullptr, nullptr, 0, nullptr}};
+                           method<dequantize>("dequantize"), method<product>("product"), method<linear>("linear"),
+                           method<setup_training>("setup_training"), method<layer_norm>("layer_norm"), method<layer_norm_backward>("layer_norm_backward"), method<embedding>("embedding"),
+                           method<embedding_backward>("embedding_backward"), method<muon>("muon"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_zc_layer_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,136 @@
+// Rows of values of three types, by pieces of eight, and sums over the lanes that share a row.  gfx950 only.
+#pragma once
+
+#include "zc_values.h"
+
+namespace zc {
+
+// Eight consecutive values as they lie in memory, at their own alignment: 32 bytes or 16.
+template <bool WIDE> struct RawEight;
+template <> struct RawEight<true> { u32 w[8]; };
+template <> struct RawEight<false> { u32 w[4]; };
+struct __attribute__((packed, aligned(4))) F32EightAt { u32 w[8]; };
+struct __attribute__((packed, aligned(2))) B16EightAt { u32 w[4]; };
+
+// The first `left` of them (8 and more: all, 0 and less: none); zeros behind.
+template <bool WIDE>
+__device__ inline RawEight<WIDE> load_eight(const void* base, u64 at, i32 left) {
+  RawEight<WIDE> r = {};
+  if (left >= 8) {
+    if constexpr (WIDE) {
+      const F32EightAt v = *reinterpret_cast<const F32EightAt*>(static_cast<const float*>(base) + at);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r.w[j] = v.w[j];
+    } else {
+      const B16EightAt v = *reinterpret_cast<const B16EightAt*>(static_cast<const u16*>(base) + at);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r.w[j] = v.w[j];
+    }
+  } else if (left > 0) {
+#pragma unroll
+    for (int j = 0; j < 7; ++j) {
+      if (j >= left) continue;
+      if constexpr (WIDE) r.w[j] = static_cast<const u32*>(base)[at + j];
+      else r.w[j / 2] |= u32(static_cast<const u16*>(base)[at + j]) << (16 * (j & 1));
+    }
+  }
+  return r;
+}
+
+// As numbers.  (Which 16-bit type it is, is the same for the whole grid.)
+template <bool WIDE>
+__device__ inline void numbers_of(const RawEight<WIDE>& r, int type, float (&v)[8]) {
+  if constexpr (WIDE) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(r.w[j]);
+  } else if (type == ZC_BF16) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(j & 1 ? r.w[j / 2] & 0xffff0000u : r.w[j / 2] << 16);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = float(__builtin_bit_cast(_Float16, u16(r.w[j / 2] >> (16 * (j & 1)))));
+  }
+}
+
+// Two numbers, each rounded once, as a word.
+template <typename ONE>
+__device__ inline u32 word_of_two(float low, float high) {
+  typedef float Two __attribute__((ext_vector_type(2)));
+  typedef ONE Pair __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(u32, __builtin_convertvector((Two{low, high}), Pair));
+}
+
+// Eight numbers, each rounded once.
+template <bool WIDE>
+__device__ inline RawEight<WIDE> rounded_eight(int type, const float (&v)[8]) {
+  RawEight<WIDE> r;
+  if constexpr (WIDE) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.w[j] = __float_as_uint(v[j]);
+  } else if (type == ZC_BF16) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r.w[j] = word_of_two<__bf16>(v[2 * j], v[2 * j + 1]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r.w[j] = word_of_two<_Float16>(v[2 * j], v[2 * j + 1]);
+  }
+  return r;
+}
+template <bool WIDE>
+__device__ inline void store_raw_eight(void* base, u64 at, i32 left, const RawEight<WIDE>& r) {
+  if (left >= 8) {
+    if constexpr (WIDE) {
+      F32EightAt v;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v.w[j] = r.w[j];
+      *reinterpret_cast<F32EightAt*>(static_cast<float*>(base) + at) = v;
+    } else {
+      B16EightAt v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v.w[j] = r.w[j];
+      *reinterpret_cast<B16EightAt*>(static_cast<u16*>(base) + at) = v;
+    }
+  } else if (left > 0) {
+#pragma unroll
+    for (int j = 0; j < 7; ++j) {
+      if (j >= left) continue;
+      if constexpr (WIDE) static_cast<u32*>(base)[at + j] = r.w[j];
+      else static_cast<u16*>(base)[at + j] = u16(r.w[j / 2] >> (16 * (j & 1)));
+    }
+  }
+}
+template <bool WIDE>
+__device__ inline void store_eight(void* base, int type, u64 at, i32 left, const float (&v)[8]) {
+  store_raw_eight<WIDE>(base, at, left, rounded_eight<WIDE>(type, v));
+}
+
+// Of a type that is known at run time only.
+__device__ inline void load_numbers(const void* base, int type, u64 at, i32 left, float (&v)[8]) {
+  if (type == ZC_F32) numbers_of<true>(load_eight<true>(base, at, left), type, v);
+  else numbers_of<false>(load_eight<false>(base, at, left), type, v);
+}
+__device__ inline void store_numbers(void* base, int type, u64 at, i32 left, const float (&v)[8]) {
+  if (type == ZC_F32) store_eight<true>(base, type, at, left, v);
+  else store_eight<false>(base, type, at, left, v);
+}
+
+// How many of a row's values there are from a piece's first on, 8 at most.
+__device__ inline i32 left_of(u64 cols, u64 col) { return col >= cols ? 0 : i32(cols - col < 8 ? cols - col : 8); }
+
+// Sums over 16 neighbouring lanes, over a wave; every lane has them, the same bits in all.
+__device__ inline float swapped(float x, u32 o) { return x + __uint_as_float(o); }
+__device__ inline float sum_of_16(float x) {
+  x = swapped(x, dpp_mov<kDppQuadSwap1>(__float_as_uint(x)));
+  x = swapped(x, dpp_mov<kDppQuadSwap2>(__float_as_uint(x)));
+  x = swapped(x, dpp_mov<kDppRowHalfMirror>(__float_as_uint(x)));
+  return swapped(x, dpp_mov<kDppRowMirror>(__float_as_uint(x)));
+}
+__device__ inline float sum_of_wave(float x) {
+  x = sum_of_16(x);
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+}  // namespace zc

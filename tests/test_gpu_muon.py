@@ -1,0 +1,195 @@
+"""The optimiser's step for matrices against its definition in 64 bits.
+
+What the operands' roundings do to X is computed, not guessed: the definition is also run in 64 bits with X, A and B rounded where the kernels round them (training_model.orthogonalised).  The
+kernels' own roundings differ from those where binary32 sums fall on the other side of a border, so that their error is of the same size, not the same: 1.5 times the model's in the 2-norm is
+allowed.  Sums in binary32 of up to K products are off by some sqrt(K) 2^-24 relative to the largest partial sums, at the five iterations' three products with a gain of at most 4 each: 2^-17 relative
+to the 2-norm covers them for the sizes here; and two parts leave 2^-22 at every rounding, far under that."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2502_18554_amd as zc
+import training_model as model
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def generator(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def values(t):
+    return t.detach().double().cpu().numpy()
+
+
+def gradient(rows, cols, g, kind="f32"):
+    """A few strong directions over weaker ones."""
+    return (torch.randn(rows, 3, generator=g, device=DEV) @ torch.randn(3, cols, generator=g, device=DEV) + torch.randn(rows, cols, generator=g, device=DEV)).mul_(0.01).to(TYPES[kind])
+
+
+def state_of(shapes):
+    return torch.zeros(zc.zc_muon_state_bytes(shapes) // 4, device=DEV)
+
+
+def workspace(shapes, wide):
+    return torch.full((zc.zc_muon_workspace_bytes(shapes, wide),), 0xFF, dtype=torch.uint8, device=DEV)
+
+
+def parts_of(state, shapes):
+    found, at = [], 0
+    for r, c in shapes:
+        found.append(state[at:at + r * c].view(r, c))
+        at += -(-r * c // 32) * 32
+    return found
+
+
+def off(got, want):
+    return np.linalg.norm(got - want) / max(np.linalg.norm(want), 1e-30)
+
+
+def allowed(u, iterations, wide):
+    exact = model.orthogonalised(u, iterations, 0)
+    return 1.5 * off(model.orthogonalised(u, iterations, 2 if wide else 1), exact) + 2.0 ** -17
+
+
+SHAPES = [(1, 1), (1, 7), (5, 3), (17, 17), (40, 30), (64, 64), (65, 130), (128, 128), (129, 257), (300, 100), (256, 512), (513, 700), (1100, 1300), (1290, 1030), (96, 4000)]
+
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("wide", [False, True])
+def test_directions(rows, cols, wide):
+    """From no weights, with a rate of one: the step is X itself."""
+    g = generator(rows + 7 * cols)
+    grad = gradient(rows, cols, g)
+    p, state = torch.zeros(rows, cols, device=DEV), state_of([(rows, cols)])
+    assert zc.zc_muon([p], [grad], state, workspace([(rows, cols)], wide), 1.0, momentum=0.0, nesterov=False, wide=wide) == 0
+    want, m = model.muon(np.zeros((rows, cols)), values(grad), np.zeros((rows, cols)), 1.0, 0.0, 0.0, 5, False)
+    assert off(values(p), want) <= allowed(values(grad), 5, wide)
+    assert np.array_equal(values(parts_of(state, [(rows, cols)])[0]), values(grad))
+
+
+@pytest.mark.parametrize("kinds", [("f32", "f32", None), ("f32", "bf16", "bf16"), ("bf16", "f16", None), ("f16", "bf16", "f32")])
+@pytest.mark.parametrize("nesterov,match_rms,wide", [(True, False, False), (False, True, True)])
+def test_steps_of_a_list(kinds, nesterov, match_rms, wide):
+    """Two steps over matrices of all kinds of shape, an empty one among them, with decay, momentum, a factor, and copies of some."""
+    kp, kg, kc = kinds
+    shapes = [(33, 65), (200, 90), (0, 5), (128, 256), (1, 50), (70, 70)]
+    g = generator(11)
+    p = [(0.1 * torch.randn(s, generator=g, device=DEV)).to(TYPES[kp]) for s in shapes]
+    copies = [torch.zeros(s, dtype=TYPES[kc], device=DEV) if i != 1 else None for i, s in enumerate(shapes)] if kc else None
+    state, ws, scale = state_of(shapes), workspace(shapes, wide), torch.full((1,), 0.6, device=DEV)
+    want, m = [values(t) for t in p], [np.zeros(s) for s in shapes]
+    for step in range(2):
+        grads = [gradient(*s, g, kg) for s in shapes]
+        assert zc.zc_muon(p, grads, state, ws, 0.2, momentum=0.9, weight_decay=0.3, nesterov=nesterov, match_rms=match_rms, wide=wide, d_copies=copies, d_grad_scale=scale) == 0
+        for i, s in enumerate(shapes):
+            if 0 in s:
+                continue
+            before, g64 = want[i], values(grads[i]) * float(np.float32(0.6))
+            want[i], m[i] = model.muon(before, g64, m[i], 0.2, 0.9, 0.3, 5, nesterov, match_rms)
+            got_m = values(parts_of(state, shapes)[i])
+            assert (np.abs(got_m - m[i]) <= 6 * (step + 1) * model.U * (np.abs(m[i]) + np.abs(g64)) + 1e-12).all()
+            u = 0.9 * m[i] + 0.1 * g64 if nesterov else m[i]
+            size = np.linalg.norm(want[i] - before * (1 - 0.2 * 0.3))
+            room = size * (allowed(u, 5, wide) + (2.0 ** -20)) + np.linalg.norm(model.half_step(kp, want[i]) + 3 * model.U * np.abs(want[i]))
+            assert np.linalg.norm(values(p[i]) - want[i]) <= room
+            if copies and copies[i] is not None:
+                # the copy is the unrounded weight rounded once: within both roundings of the stored one
+                assert (np.abs(values(copies[i]) - values(p[i])) <= model.half_step(kc, values(p[i])) * 1.01 + model.half_step(kp, values(p[i])) * 1.01).all()
+            want[i], m[i] = values(p[i]), got_m.copy()            # (the next step begins where this one ended)
+
+
+@pytest.mark.parametrize("iterations", [1, 2, 3, 8])
+def test_iterations(iterations):
+    g = generator(iterations)
+    grad = gradient(90, 150, g)
+    for wide in (False, True):
+        p = torch.zeros(90, 150, device=DEV)
+        assert zc.zc_muon([p], [grad], state_of([(90, 150)]), workspace([(90, 150)], wide), 1.0, momentum=0.0, nesterov=False, wide=wide, iterations=iterations) == 0
+        assert off(values(p), -model.orthogonalised(values(grad), iterations, 0)) <= allowed(values(grad), iterations, wide)
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-12, 1e25, 3e38])
+def test_magnitudes(size):
+    """Gradients far from one; ones so small that the norm's floor holds them; and none at all."""
+    g = generator(1)
+    grad = torch.rand(50, 60, generator=g, device=DEV).sub_(0.5).mul_(size)
+    p = torch.zeros(50, 60, device=DEV)
+    assert zc.zc_muon([p], [grad], state_of([(50, 60)]), workspace([(50, 60)], True), 1.0, momentum=0.0, nesterov=False, wide=True) == 0
+    want = -model.orthogonalised(values(grad), 5, 0)
+    assert np.abs(values(p) - want).max() <= 2.0 ** -12 * max(np.abs(want).max(), 2.0 ** -20)       # (under the floor X is so small that binary16 at 2^12 has few bits: 2^-37 of it at least)
+    q = torch.full((50, 60), 0.5, device=DEV)
+    assert zc.zc_muon([q], [torch.zeros_like(grad)], state_of([(50, 60)]), workspace([(50, 60)], False), 0.5, weight_decay=0.5) == 0
+    assert bool((q == 0.375).all())
+
+
+def test_what_is_not_finite_keeps_to_its_matrix():
+    g = generator(2)
+    grads = [gradient(40, 50, g) for _ in range(3)]
+    shapes = [(40, 50)] * 3
+    clean, p = [torch.zeros(40, 50, device=DEV) for _ in range(3)], [torch.zeros(40, 50, device=DEV) for _ in range(3)]
+    ws = workspace(shapes, False)
+    assert zc.zc_muon(clean, grads, state_of(shapes), ws, 1.0) == 0
+    grads[1][3, 4] = float("nan")
+    assert zc.zc_muon(p, grads, state_of(shapes), ws, 1.0) == 0
+    assert torch.equal(p[0], clean[0]) and torch.equal(p[2], clean[2]) and bool(p[1].isnan().all())
+
+
+def test_a_factor_that_is_not_finite_changes_nothing():
+    g = generator(3)
+    shapes = [(70, 40), (64, 64)]
+    p = [torch.randn(s, generator=g, device=DEV) for s in shapes]
+    copies = [torch.full(s, 4.0, device=DEV) for s in shapes]
+    state = torch.randn(zc.zc_muon_state_bytes(shapes) // 4, generator=g, device=DEV)
+    before = [t.clone() for t in (*p, *copies, state)]
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        assert zc.zc_muon(p, [gradient(*s, g) for s in shapes], state, workspace(shapes, True), 0.1, d_copies=copies, d_grad_scale=torch.full((1,), bad, device=DEV), wide=True) == 0
+    assert all(torch.equal(a, b) for a, b in zip((*p, *copies, state), before))
+
+
+def test_more_matrices_than_a_launch_takes():
+    g = generator(4)
+    shapes = [(3 + i % 5, 2 + i % 7) for i in range(150)]
+    grads = [gradient(*s, g) for s in shapes]
+    p = [torch.zeros(s, device=DEV) for s in shapes]
+    assert zc.zc_muon(p, grads, state_of(shapes), workspace(shapes, True), 1.0, momentum=0.0, nesterov=False, wide=True) == 0
+    for i in (0, 63, 64, 127, 128, 149):
+        want, _ = model.muon(np.zeros(shapes[i]), values(grads[i]), 0, 1.0, 0.0, 0.0, 5, False)
+        assert off(values(p[i]), want) <= allowed(values(grads[i]), 5, True)
+
+
+def test_graph_streams_and_other_ways(monkeypatch):
+    g = generator(5)
+    shapes = [(130, 200), (200, 70), (64, 64)]
+    grads = [gradient(*s, g) for s in shapes]
+
+    def make():
+        return dict(p=[torch.ones(s, device=DEV) for s in shapes], state=state_of(shapes), ws=workspace(shapes, False))
+
+    def call(t, **how):
+        assert zc.zc_muon(t["p"], grads, t["state"], t["ws"], 0.1, weight_decay=0.1, **how) == 0
+
+    same = lambda a, b: all(torch.equal(x, y) for x, y in zip((*a["p"], a["state"]), (*b["p"], b["state"])))
+    eager, captured, other, by_ctypes = make(), make(), make(), make()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        call(captured)
+    for _ in range(3):
+        graph.replay()
+        call(eager)
+        torch.cuda.synchronize()
+        assert same(captured, eager)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        call(other, stream=side)
+    torch.cuda.synchronize()
+    assert same(other, eager)
+    monkeypatch.setattr(zc.binding, "_native_layers", None)
+    for _ in range(3):
+        call(by_ctypes)
+    assert same(by_ctypes, eager)
