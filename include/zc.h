@@ -409,7 +409,7 @@ int zc_embedding_backward(const void* d_dy, int dy_type, size_t dy_stride, const
 /* One optimiser step over k matrices (rows[i] x cols[i] values in one piece; host arrays of k entries) whose momentum is made nearly orthogonal (Jordan et al., "Muon", 2024).
  * In binary32, with X the matrix, turned where it has more rows than columns:
  *   g = grad x *d_grad_scale;  m' = momentum m + (1 - momentum) g;  u = momentum m' + (1 - momentum) g with ZC_MUON_NESTEROV, m' without
- *   X = u / max(root of the sum of u^2, 1e-7);  `iterations` times:  A = X X^T,  B = -4.7750 A + 2.0315 A A,  X = 3.4445 X + B X
+ *   X = u / max(root of the sum of u^2, 1e-7);  `iterations` times:  A = X X^T,  B = 3.4445 I - 4.7750 A + 2.0315 A A,  X = B X
  *   p' = p (1 - lr weight_decay) - lr factor X
  * factor: sqrt(max(1, rows / cols)); with ZC_MUON_MATCH_RMS 0.2 sqrt(max(rows, cols)).
  * The products' operands are X, A and B rounded to 11 bits (binary16, scaled by 2^12), with ZC_MUON_WIDE to 22 bits (two of them; three times the work), sums are in

@@ -128,34 +128,41 @@ u64 muon_tiles(const MuonTensor& t, int mode, u64 side) {
   const u64 down = (t.r + side - 1) / side, across = (t.c + side - 1) / side;
   return mode == kMuonGram || mode == kMuonPoly ? down * (down + 1) / 2 : down * across;
 }
+constexpr int muon_stages(int T) { return T == 4 ? 2 : T == 3 ? 3 : T == 2 ? 2 : 4; }        // that lie in LDS
 template <int T, int MODE>
 void launch_muon_product(MuonArgs& a, hipStream_t stream) {
   a.count = 0;
   for (u32 i = 0; i < a.tensors; ++i) {
-    a.t[i].first = a.count;
+    a.first[i] = a.count;
     a.count += u32(muon_tiles(a.t[i], MODE, 64 * T));
   }
-  const u32 at_once = 256 * (T == 4 ? 1 : T == 2 ? 2 : 4);
-  hipLaunchKernelGGL((muon_product_kernel<T, MODE>), dim3(a.count < at_once ? a.count : at_once), dim3(256), 0, stream, a);
+  const u32 at_once = 256 * muon_groups(T, 64, muon_stages(T));
+  hipLaunchKernelGGL((muon_product_kernel<T, 64, muon_stages(T), MODE>), dim3(a.count < at_once ? a.count : at_once), dim3(256), 0, stream, a);
 }
-// The size of tile that takes the least time, in us, by what a tile takes: its begin and end, and a stage of 64 values.
+// The size of tile that takes the least time, in us, by what a turn of all CUs has been measured to take: a tile's begin and end, and its stages of 64 values.
 template <int MODE>
 void launch_muon_product(MuonArgs& a, hipStream_t stream) {
-  double large = 0, middle = 0, small = 0;
-  u64 tiles[3] = {0, 0, 0};
-  double stages = 0;
+  double tiles[4] = {}, along[4] = {};
   for (u32 i = 0; i < a.tensors; ++i) {
-    for (int t = 0; t < 3; ++t) tiles[t] += muon_tiles(a.t[i], MODE, u64(64) << t);
-    const double of_this = double(muon_along(MODE == kMuonGram ? a.t[i].c : a.t[i].r)) / 64 * (a.planes > 1 ? 3 : 1);
-    if (of_this > stages) stages = of_this;
+    const double stages = double(muon_along(MODE == kMuonGram ? a.t[i].c : a.t[i].r)) / 64 * (a.planes > 1 ? 3 : 1);
+    for (int t = 0; t < 4; ++t) {
+      const double of_this = double(muon_tiles(a.t[i], MODE, u64(64) * (t + 1)));
+      tiles[t] += of_this;
+      along[t] += of_this * stages;
+    }
   }
-  const auto turns = [&](int t) { return double((tiles[t] + 255) / 256); };
-  large = turns(2) * (5.0 + 1.0 * stages);
-  middle = 3.0 + turns(1) * (1.0 + 0.3 * stages);
-  small = 3.0 + turns(0) * (0.4 + 0.1 * stages);
-  if (large <= middle && large <= small) launch_muon_product<4, MODE>(a, stream);
-  else if (middle <= small) launch_muon_product<2, MODE>(a, stream);
-  else launch_muon_product<1, MODE>(a, stream);
+  const auto stages = [&](int t) { return along[t] / tiles[t]; };
+  const double cost[4] = {3 + std::ceil(tiles[0] / 512) * (2 + 0.25 * stages(0)),
+                          4 + (tiles[1] <= 256 ? 2 + 0.6 * stages(1) : std::ceil(tiles[1] / 512) * (10 + 0.92 * stages(1))),
+                          std::ceil(tiles[2] / 256) * (12 + 0.83 * stages(2)),
+                          std::ceil(tiles[3] / 256) * (22 + (tiles[3] <= 160 ? 1.15 : 1.45) * stages(3))};
+  int best = 0;
+  for (int t = 1; t < 4; ++t)
+    if (cost[t] < cost[best]) best = t;
+  if (best == 0) launch_muon_product<1, MODE>(a, stream);
+  else if (best == 1) launch_muon_product<2, MODE>(a, stream);
+  else if (best == 2) launch_muon_product<3, MODE>(a, stream);
+  else launch_muon_product<4, MODE>(a, stream);
 }
 
 // A launch of `groups(i)` workgroups for matrix i.
@@ -163,7 +170,7 @@ template <typename K, typename F>
 void launch_muon(K kernel, MuonArgs& a, const F& groups, hipStream_t stream) {
   a.count = 0;
   for (u32 i = 0; i < a.tensors; ++i) {
-    a.t[i].first = a.count;
+    a.first[i] = a.count;
     a.count += u32(groups(a.t[i]));
   }
   if (a.count) hipLaunchKernelGGL(kernel, dim3(a.count), dim3(256), 0, stream, a);
@@ -325,7 +332,7 @@ int zc_muon(int k, const size_t* rows, const size_t* cols, void* const* d_params
         t.r = smaller(r, c), t.c = larger(r, c);
         const double factor = flags & ZC_MUON_MATCH_RMS ? 0.2 * std::sqrt(double(t.c)) : r > c ? std::sqrt(double(r) / double(c)) : 1.0;
         t.step = float(lr * factor);
-        if (r > c) a.turned[a.tensors / 32] |= 1u << (a.tensors % 32);
+        t.turned = r > c;
         ++a.tensors;
       }
       m += muon_padded(r * c);
@@ -340,7 +347,7 @@ int zc_muon(int k, const size_t* rows, const size_t* cols, void* const* d_params
     }
     launch_muon(muon_momentum_kernel, a, [](const MuonTensor& t) { return muon_partials(u64(t.r) * t.c); }, stream);
     launch_muon(muon_begin_kernel, a, [](const MuonTensor& t) { return muon_along(t.r) / 64 * (muon_along(t.c) / 64); }, stream);
-    if (padded) launch_muon(muon_zeros_kernel, a, [](const MuonTensor& t) { return (t.c + 255) / 256; }, stream);
+    if (padded) launch_muon(muon_zeros_kernel, a, [](const MuonTensor& t) { return (t.c + 15) / 16; }, stream);
     for (int n = 0; n < iterations; ++n) {
       launch_muon_product<kMuonGram>(a, stream);
       launch_muon_product<kMuonPoly>(a, stream);

@@ -67,8 +67,8 @@ def orthogonalised(u, iterations, parts):
     x = rounded(x / max(np.sqrt((x * x).sum()), 1e-7), parts)
     for i in range(iterations):
         a = rounded(x @ x.T, parts)
-        b = rounded(B * a + C * (a @ a), parts)
-        x = A * x + b @ x
+        b = rounded(A * np.eye(len(a)) + B * a + C * (a @ a), parts)
+        x = b @ x
         if i + 1 < iterations:
             x = rounded(x, parts)
     return x.T if turned else x
