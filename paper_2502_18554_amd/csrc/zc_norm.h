@@ -76,8 +76,6 @@ __global__ __launch_bounds__(norm_threads<T>()) void norm_kernel(NormArgs a) {
     left[p] = left_of(a.cols, col);
 #pragma unroll
     for (int j = 0; j < 8; ++j) w[p][j] = 1.0f, b[p][j] = 0.0f;
-    if (a.w) load_numbers(a.w, a.w_type, col, left[p], w[p]);
-    if (a.b) load_numbers(a.b, a.w_type, col, left[p], b[p]);
   }
   const u64 step = u64(gridDim.x) * ROWS;
   u64 row = u64(blockIdx.x) * ROWS + group;
@@ -87,6 +85,8 @@ __global__ __launch_bounds__(norm_threads<T>()) void norm_kernel(NormArgs a) {
     for (int p = 0; p < P; ++p) next[p] = load_eight<X32>(a.x, r * a.x_stride + u64(8) * (u32(p) * T + t), r < a.rows ? left[p] : 0);
   };
   ask(row);
+  if (a.w) load_pieces<P>(a.w, a.w_type, 8 * t, 8 * T, left, w);
+  if (a.b) load_pieces<P>(a.b, a.w_type, 8 * t, 8 * T, left, b);
   u32 parity = 0;
   for (u64 first = u64(blockIdx.x) * ROWS; first < a.rows; first += step, row += step) {       // (the same for all threads)
     float x[P][8];
@@ -160,10 +160,11 @@ __global__ __launch_bounds__(norm_threads<T>()) void norm_backward_kernel(NormBa
     left[p] = left_of(a.cols, col);
 #pragma unroll
     for (int j = 0; j < 8; ++j) w[p][j] = 1.0f, dw[p][j] = 0.0f, db[p][j] = 0.0f;
-    if (a.w) load_numbers(a.w, a.w_type, col, left[p], w[p]);
   }
   const u64 step = u64(gridDim.x) * ROWS;
   u64 row = u64(blockIdx.x) * ROWS + group;
+  // (Two rows of 32-bit values of this length do not fit into the registers of two waves.)
+  constexpr bool AHEAD = !(T == 512 && (X32 || DY32));
   RawEight<X32> next_x[P];
   RawEight<DY32> next_dy[P];
   float next_mean, next_d;
@@ -178,17 +179,26 @@ __global__ __launch_bounds__(norm_threads<T>()) void norm_backward_kernel(NormBa
     next_mean = there ? a.stats[r] : 0.0f;
     next_d = there ? a.stats[a.rows + r] : 0.0f;
   };
-  ask(row);
+  if constexpr (P <= 2) {
+    if (a.w) load_pieces<P>(a.w, a.w_type, 8 * t, 8 * T, left, w);
+  } else if (a.w) {                                        // (one by one: the registers are full)
+#pragma unroll
+    for (int p = 0; p < P; ++p) load_numbers(a.w, a.w_type, u64(8) * (u32(p) * T + t), left[p], w[p]);
+  }
+  if (AHEAD) ask(row);
   u32 parity = 0;
   for (u64 first = u64(blockIdx.x) * ROWS; first < a.rows; first += step, row += step) {
     float z[P][8], dy[P][8];
+    if (!AHEAD) ask(row);
     const float mean = next_mean, d = next_d;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       numbers_of<X32>(next_x[p], a.x_type, z[p]);
       numbers_of<DY32>(next_dy[p], a.dy_type, dy[p]);
     }
-    ask(row + step);
+    if (AHEAD) ask(row + step);
+    float old[P <= 2 ? P : 1][8];                          // what dx is added to
+    if constexpr (P <= 2) if (a.dx && a.add && row < a.rows) load_pieces<P>(a.dx, a.dx_type, row * a.dx_stride + 8 * t, 8 * T, left, old);
     float one = 0.0f, two = 0.0f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -222,11 +232,11 @@ __global__ __launch_bounds__(norm_threads<T>()) void norm_backward_kernel(NormBa
       for (int p = 0; p < P; ++p) {
         const u64 at = row * a.dx_stride + u64(8) * (u32(p) * T + t);
         float v[8];
-        if (a.add) load_numbers(a.dx, a.dx_type, at, left[p], v);
+        if (P > 2 && a.add) load_numbers(a.dx, a.dx_type, at, left[p], old[0]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float g = d * (__builtin_fmaf(dy[p][j], w[p][j], -one) - z[p][j] * two);
-          v[j] = a.add ? v[j] + g : g;
+          v[j] = a.add ? old[P <= 2 ? p : 0][j] + g : g;
         }
         store_numbers(a.dx, a.dx_type, at, left[p], v);
       }

@@ -114,6 +114,21 @@ __device__ inline void store_numbers(void* base, int type, u64 at, i32 left, con
   else store_eight<false>(base, type, at, left, v);
 }
 
+// P pieces of a row, `apart` values from one to the next: all of them are asked for before the first is looked at, also where the type is known at run time only.
+template <bool WIDE, int P>
+__device__ inline void load_pieces_of(const void* base, int type, u64 at, u64 apart, const i32 (&left)[P], float (&v)[P][8]) {
+  RawEight<WIDE> raw[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p) raw[p] = load_eight<WIDE>(base, at + p * apart, left[p]);
+#pragma unroll
+  for (int p = 0; p < P; ++p) numbers_of<WIDE>(raw[p], type, v[p]);
+}
+template <int P>
+__device__ inline void load_pieces(const void* base, int type, u64 at, u64 apart, const i32 (&left)[P], float (&v)[P][8]) {
+  if (type == ZC_F32) load_pieces_of<true, P>(base, type, at, apart, left, v);
+  else load_pieces_of<false, P>(base, type, at, apart, left, v);
+}
+
 // How many of a row's values there are from a piece's first on, 8 at most.
 __device__ inline i32 left_of(u64 cols, u64 col) { return col >= cols ? 0 : i32(cols - col < 8 ? cols - col : 8); }
 

@@ -152,9 +152,9 @@ void launch_muon_product(MuonArgs& a, hipStream_t stream) {
     }
   }
   const auto stages = [&](int t) { return along[t] / tiles[t]; };
-  const double cost[4] = {3 + std::ceil(tiles[0] / 512) * (2 + 0.25 * stages(0)),
-                          4 + (tiles[1] <= 256 ? 2 + 0.6 * stages(1) : std::ceil(tiles[1] / 512) * (10 + 0.92 * stages(1))),
-                          std::ceil(tiles[2] / 256) * (12 + 0.83 * stages(2)),
+  const double cost[4] = {3 + (tiles[0] <= 256 ? 2 + 0.25 * stages(0) : std::ceil(tiles[0] / 512) * (1.5 + 0.4 * stages(0))),
+                          tiles[1] <= 256 ? 9 + 0.6 * stages(1) : 4 + std::ceil(tiles[1] / 512) * (12 + 1.1 * stages(1)),
+                          std::ceil(tiles[2] / 256) * (12 + (tiles[2] <= 160 ? 0.68 : 0.85) * stages(2)),
                           std::ceil(tiles[3] / 256) * (22 + (tiles[3] <= 160 ? 1.15 : 1.45) * stages(3))};
   int best = 0;
   for (int t = 1; t < 4; ++t)
@@ -194,7 +194,7 @@ int zc_layer_norm(const void* d_x, int x_type, size_t rows, size_t cols, size_t 
   }
   by_cols(cols, [&](auto lanes, auto pieces) {
     constexpr int T = decltype(lanes)::value, P = decltype(pieces)::value, W = norm_threads<T>();
-    const dim3 grid(at_most((rows + W / T - 1) / (W / T), W == 256 ? 2048 : 512));
+    const dim3 grid(at_most((rows + W / T - 1) / (W / T), W == 256 ? 2048 : 256));
     if (x_type == ZC_F32) hipLaunchKernelGGL((norm_kernel<T, P, true>), grid, dim3(W), 0, stream, a);
     else hipLaunchKernelGGL((norm_kernel<T, P, false>), grid, dim3(W), 0, stream, a);
   });
@@ -273,13 +273,15 @@ int zc_embedding_backward(const void* d_dy, int dy_type, size_t dy_stride, const
   const dim3 groups(1u << plan.groups_log2);
   if (token_bits == 32) hipLaunchKernelGGL(token_order_kernel<32>, groups, dim3(64 * kTokenWaves), 0, stream, t);
   else hipLaunchKernelGGL(token_order_kernel<64>, groups, dim3(64 * kTokenWaves), 0, stream, t);
-  const EmbeddingBackwardArgs a{d_dy, place, row, first, reinterpret_cast<float*>(ws + plan.at_partial), d_grad, table_rows, cols, dy_stride, grad_stride, float(scale), dy_type, grad_type,
-                                add ? 1u : 0u, plan.chunk_log2, plan.per << plan.groups_log2, plan.per, plan.groups_log2, plan.pieces};
-  const u32 zeros = add ? 0 : (a.slots + kZeroRows - 1) / kZeroRows;
-  const dim3 grid(plan.pieces + zeros, u32((cols + 2047) / 2048));
-  if (dy_type == ZC_F32) hipLaunchKernelGGL(embedding_sums_kernel<true>, grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL(embedding_sums_kernel<false>, grid, dim3(256), 0, stream, a);
-  if (plan.pieces > 1) hipLaunchKernelGGL(embedding_joins_kernel, dim3(plan.pieces, u32((cols + 255) / 256)), dim3(256), 0, stream, a);
+  const u32 slots = plan.per << plan.groups_log2, zeros = add ? 0 : (slots + kZeroRows - 1) / kZeroRows, groups_of_sums = plan.pieces + zeros;
+  const EmbeddingBackwardArgs a{d_dy, place, row, first, reinterpret_cast<float*>(ws + plan.at_partial), d_grad, n, table_rows, cols, dy_stride, grad_stride, float(scale), dy_type, grad_type,
+                                add ? 1u : 0u, plan.chunk_log2, slots, plan.per, plan.groups_log2, ((u64(zeros) << 32) + groups_of_sums - 1) / groups_of_sums};
+  const dim3 grid(groups_of_sums, u32((cols + 2047) / 2048)), threads(cols > 1536 ? 256 : u32((cols + 511) / 512) * 64);
+  if (dy_type == ZC_F32 && add) hipLaunchKernelGGL((embedding_sums_kernel<true, true>), grid, threads, 0, stream, a);
+  else if (dy_type == ZC_F32) hipLaunchKernelGGL((embedding_sums_kernel<true, false>), grid, threads, 0, stream, a);
+  else if (add) hipLaunchKernelGGL((embedding_sums_kernel<false, true>), grid, threads, 0, stream, a);
+  else hipLaunchKernelGGL((embedding_sums_kernel<false, false>), grid, threads, 0, stream, a);
+  if (plan.pieces > 1) hipLaunchKernelGGL(embedding_joins_kernel, dim3((plan.pieces + kJoinPieces - 1) / kJoinPieces, u32((cols + 255) / 256)), dim3(64 * kJoinWaves), 0, stream, a);
   return launched();
 }
 
