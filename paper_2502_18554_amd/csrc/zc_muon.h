@@ -44,10 +44,13 @@ struct MuonTensor {
   u32 turned;
 };
 struct MuonArgs {
-  MuonTensor t[kMuonTensors];
-  u32 first[kMuonTensors];       // of its tiles (or workgroups) in the launch, in ascending order
-  u32 tensors;
+  // What the waves need first (they have it in registers when they start).  Where all matrices have one shape, what a tile needs to begin is here, and not behind two answers of memory.
   u32 count;                     // tiles (or workgroups) of the launch
+  u32 each;                      // of a matrix, where all have one shape; 0 otherwise
+  u32 r, c;                      // that shape
+  u8* at;                        // the first matrix's share of the workspace, `bytes` before the next one's
+  u64 bytes;
+  u32 tensors;
   u32 planes;                    // 1 or 2
   u32 which;                     // of the two turned X
   const float* grad_scale;
@@ -55,8 +58,11 @@ struct MuonArgs {
   float keep, mu, rest;          // 1 - lr decay; mu, 1 - mu
   u32 nesterov;
   int param_type, grad_type, copy_type;
+  u32 first[kMuonTensors];       // of its tiles (or workgroups) in the launch, in ascending order
+  MuonTensor t[kMuonTensors];
 };
 static_assert(sizeof(MuonArgs) <= 4096);
+// (The kernels read them where they lie: of a parameter that is used in many places, with an index, the compiler makes a copy in scratch memory.)
 
 // Places of a matrix's parts in its share of the workspace: X, X turned twice (one is read while the other is written), A, B; the low parts of two behind the high ones of each.
 struct MuonParts {
@@ -77,10 +83,24 @@ struct MuonParts {
 
 // The matrix that a tile or workgroup belongs to: a lane looks at one of them each, since a search one by one would wait for memory at each (24 matrices of 256 x 512: 4 us a launch).
 static_assert(kMuonTensors == 64);
-__device__ inline u32 muon_tensor_of(const MuonArgs& a, u32 tile) {
-  const u32 lane = threadIdx.x & 63u;
-  return u32(__popcll(__ballot(lane < a.tensors && a.first[lane] <= tile))) - 1;
-}
+struct MuonOf {
+  u32 i, r, c, first;            // the matrix, its shape and its first tile
+  u8* at;
+  __device__ MuonOf(const MuonArgs& a, u32 tile) {
+    if (a.each) {
+      i = tile / a.each;
+      first = i * a.each;
+      r = a.r, c = a.c;
+      at = a.at + i * a.bytes;
+    } else {
+      const u32 lane = threadIdx.x & 63u;
+      i = u32(__popcll(__ballot(lane < a.tensors && a.first[lane] <= tile))) - 1;
+      first = a.first[i];
+      r = a.t[i].r, c = a.t[i].c;
+      at = a.t[i].at;
+    }
+  }
+};
 
 // ---- Momentum, and the sum of u's squares: in 64 bits, by workgroups whose sums the next launch adds.
 constexpr u32 kMuonPartials = 512;
@@ -98,12 +118,14 @@ __device__ inline double sum_of_256(double x, double (&slot)[4]) {
   return (slot[0] + slot[1]) + (slot[2] + slot[3]);
 }
 
-__global__ __launch_bounds__(256) void muon_momentum_kernel(MuonArgs a) {
+__global__ __launch_bounds__(256) void muon_momentum_kernel(MuonArgs) {
+  const MuonArgs& a = kernel_args<MuonArgs, 0>();
   __shared__ double slot[4];
   const float scale = a.grad_scale ? *a.grad_scale : 1.0f;
   if (!(fabsf(scale) < __builtin_inff())) return;
-  const u32 i = muon_tensor_of(a, blockIdx.x), part = blockIdx.x - a.first[i];
-  const u64 values = u64(a.t[i].r) * a.t[i].c;
+  const MuonOf of(a, blockIdx.x);
+  const u32 i = of.i, part = blockIdx.x - of.first;
+  const u64 values = u64(of.r) * of.c;
   const u32 parts = muon_partials(values);
   double sum = 0.0;
   for (u64 at = u64(part) * kMuonPiece + 8 * threadIdx.x; at < values; at += u64(parts) * kMuonPiece) {
@@ -131,15 +153,17 @@ __device__ inline void halves_of(float v, u32 planes, _Float16& high, _Float16& 
 }
 
 // ---- X, as it is and turned, from m' and the gradient: tiles of 64 x 64 of the matrix as it lies in memory.
-__global__ __launch_bounds__(256) void muon_begin_kernel(MuonArgs a) {
+__global__ __launch_bounds__(256) void muon_begin_kernel(MuonArgs) {
+  const MuonArgs& a = kernel_args<MuonArgs, 0>();
   __shared__ double slot[4];
   __shared__ float tile[64][65];
   const float scale = a.grad_scale ? *a.grad_scale : 1.0f;
-  const u32 i = muon_tensor_of(a, blockIdx.x), r = a.t[i].r, c = a.t[i].c;
+  const MuonOf of(a, blockIdx.x);
+  const u32 i = of.i, r = of.r, c = of.c;
   const bool turn = a.t[i].turned;
   const u64 rows = turn ? c : r, cols = turn ? r : c;
   const MuonParts parts(r, c, a.planes);
-  const u32 across = u32(muon_along(cols) / 64), t = blockIdx.x - a.first[i];
+  const u32 across = u32(muon_along(cols) / 64), t = blockIdx.x - of.first;
   const u64 row0 = u64(t / across) * 64, col0 = u64(t % across) * 64;
   const u32 n = muon_partials(rows * cols);
   double sum = 0.0;
@@ -166,7 +190,7 @@ __global__ __launch_bounds__(256) void muon_begin_kernel(MuonArgs a) {
       high[j] = one, low[j] = two;
     }
     if (row < rows) {
-      u8* const place = a.t[i].at + to + 2 * (row * along + col);
+      u8* const place = of.at + to + 2 * (row * along + col);
       *reinterpret_cast<f16x8_t*>(place) = high;
       if (a.planes > 1) *reinterpret_cast<f16x8_t*>(place + plane) = low;
     }
@@ -184,7 +208,7 @@ __global__ __launch_bounds__(256) void muon_begin_kernel(MuonArgs a) {
       high[j] = one, low[j] = two;
     }
     if (col < cols && row < along_2) {
-      u8* const place = a.t[i].at + to_2 + 2 * (col * along_2 + row);
+      u8* const place = of.at + to_2 + 2 * (col * along_2 + row);
       *reinterpret_cast<f16x8_t*>(place) = high;
       if (a.planes > 1) *reinterpret_cast<f16x8_t*>(place + plane_2) = low;
     }
@@ -192,15 +216,17 @@ __global__ __launch_bounds__(256) void muon_begin_kernel(MuonArgs a) {
 }
 
 // Zeros behind the rows of A, B and the other X turned: the products write values only.  A thread has eight of the last 128 values of a row, as far as they are behind its end.
-__global__ __launch_bounds__(256) void muon_zeros_kernel(MuonArgs a) {
-  const u32 i = muon_tensor_of(a, blockIdx.x), r = a.t[i].r, c = a.t[i].c;
+__global__ __launch_bounds__(256) void muon_zeros_kernel(MuonArgs) {
+  const MuonArgs& a = kernel_args<MuonArgs, 0>();
+  const MuonOf of(a, blockIdx.x);
+  const u32 r = of.r, c = of.c;
   const MuonParts parts(r, c, a.planes);
-  const u64 row = u64(blockIdx.x - a.first[i]) * 16 + threadIdx.x / 16, col = parts.row_t - kMuonAlong + 8 * (threadIdx.x % 16);
+  const u64 row = u64(blockIdx.x - of.first) * 16 + threadIdx.x / 16, col = parts.row_t - kMuonAlong + 8 * (threadIdx.x % 16);
   if (col + 8 <= r || row >= c) return;
   const u32 skip = col < r ? r - u32(col) : 0;
   const auto clear = [&](u64 from, u64 plane) {
     for (u32 k = 0; k < a.planes; ++k) {
-      _Float16* const to = reinterpret_cast<_Float16*>(a.t[i].at + from + k * plane) + row * parts.row_t + col;
+      _Float16* const to = reinterpret_cast<_Float16*>(of.at + from + k * plane) + row * parts.row_t + col;
       if (skip == 0) *reinterpret_cast<f16x8_t*>(to) = f16x8_t{};
       else for (u32 j = skip; j < 8; ++j) to[j] = _Float16(0.0f);
     }
@@ -262,11 +288,22 @@ struct MuonTiles {
   // Row and column of tile t of a matrix whose results are `down` x `across` tiles.
   __device__ static void place(u32 t, u32 down, u32 across, u32& row, u32& col) {
     if constexpr (kTriangle) {
-      u32 i = u32((sqrtf(8.0f * float(t) + 1.0f) - 1.0f) * 0.5f);
-      while (i * (i + 1) / 2 > t) --i;
-      while ((i + 1) * (i + 2) / 2 <= t) ++i;
-      row = uniform(i);
-      col = uniform(t - i * (i + 1) / 2);
+      // Strips of eight rows of tiles, down their columns: 32 s^2 + 4 s tiles are before strip s, which has 8 s whole columns and a triangle.
+      u32 s = u32(sqrtf(float(t) * (1.0f / 32.0f)));
+      while (s && 32 * s * s + 4 * s > t) --s;
+      while (32 * (s + 1) * (s + 1) + 4 * (s + 1) <= t) ++s;
+      u32 rest = t - (32 * s * s + 4 * s), c = 0;
+      const u32 high = min(8u, down - 8u * s);
+      if (rest < 8u * s * high) {
+        c = rest / high;
+        row = uniform(8u * s + rest - c * high);
+        col = uniform(c);
+      } else {
+        rest -= 8u * s * high;
+        while (rest >= high - c) rest -= high - c++;
+        row = uniform(8u * s + c + rest);
+        col = uniform(8u * s + c);
+      }
     } else {
       const u32 strip = t / (8u * across), rest = t - strip * 8u * across, high = min(8u, down - 8u * strip), c = rest / high;
       col = uniform(c);
@@ -286,47 +323,180 @@ __device__ inline void sixteen_to_memory(u32 (&w)[8]) {
 #pragma unroll
   for (int d = 0; d < 4; ++d) swap_sixteens(w[d], w[4 + d]);
 }
-struct MuonPlace {                                   // of a lane's two pieces
-  u64 at[2];
-  bool there[2];
-};
-__device__ inline void read_sixteen(const u8* from, const MuonPlace& place, u32 (&w)[8]) {
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const u32x4_t p = place.there[q] ? *reinterpret_cast<const u32x4_t*>(from + place.at[q]) : u32x4_t{};
-#pragma unroll
-    for (int d = 0; d < 4; ++d) w[4 * q + d] = p[d];
-  }
-}
 __device__ inline float half_of(const u32 (&w)[8], int k) { return float(__builtin_bit_cast(_Float16, u16(w[k / 2] >> (16 * (k & 1))))); }
-__device__ inline void write_sixteen(u8* to, const MuonPlace& place, u32 (&w)[8]) {
-  sixteen_to_memory(w);
-#pragma unroll
-  for (int q = 0; q < 2; ++q)
-    if (place.there[q]) *reinterpret_cast<u32x4_t*>(to + place.at[q]) = u32x4_t{w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]};
-}
-// The same values turned: four lanes exchange theirs so that each has four neighbouring rows of one column, 8 bytes, for four times four columns.
-// `at`: of row 4 (l % 32 / 4), column 16 (l / 32) + l % 4, in the turned matrix; rows: how many from there; left: how many of the columns there are from the first on.
-__device__ inline void write_turned(u8* at, u64 along, i32 rows, i32 left, u32 lane, const u32 (&w)[8]) {
-  const bool upper = lane & 2u, odd = lane & 1u;
-  const u32 give = odd ? 0x01000504u : 0x03020706u, first = odd ? 0x07060100u : 0x01000504u, second = odd ? 0x07060302u : 0x03020504u;
-#pragma unroll
-  for (int m = 0; m < 4; ++m) {
-    const u32 other = dpp_mov<kDppQuadSwap2>(upper ? w[2 * m] : w[2 * m + 1]);
-    const u32 p = upper ? other : w[2 * m], r = upper ? w[2 * m + 1] : other;         // rows (lane & 1) and that + 2, two columns
+
+// The same values turned: four lanes exchange theirs so that each has four neighbouring rows of one column, two words, for four times four columns.
+struct MuonTurn {
+  u32 give, first, second;                           // which bytes
+  bool upper;
+  __device__ explicit MuonTurn(u32 lane) {
+    const bool odd = lane & 1u;
+    upper = lane & 2u;
+    give = odd ? 0x01000504u : 0x03020706u, first = odd ? 0x07060100u : 0x01000504u, second = odd ? 0x07060302u : 0x03020504u;
+  }
+  __device__ u32x2_t operator()(u32 low, u32 high) const {
+    const u32 other = dpp_mov<kDppQuadSwap2>(upper ? low : high);
+    const u32 p = upper ? other : low, r = upper ? high : other;              // rows (lane & 1) and that + 2, two columns
     const u32 got = dpp_mov<kDppQuadSwap1>(__builtin_amdgcn_perm(p, r, give));
-    const u32 one = __builtin_amdgcn_perm(p, got, first), two = __builtin_amdgcn_perm(r, got, second);
-    if (4 * m + i32(lane & 3u) < left && rows > 0) {
-      u8* const to = at + 2 * along * (4 * m);
-      if (rows >= 4) {
-        *reinterpret_cast<u32x2_t*>(to) = u32x2_t{one, two};
-      } else {
-        *reinterpret_cast<u16*>(to) = u16(one);
-        if (rows > 1) *reinterpret_cast<u16*>(to + 2) = u16(one >> 16);
-        if (rows > 2) *reinterpret_cast<u16*>(to + 4) = u16(two);
+    return u32x2_t{__builtin_amdgcn_perm(p, got, first), __builtin_amdgcn_perm(r, got, second)};
+  }
+};
+
+// The results of a wave, 32 T x 32 T from (row0, col0) on.  mirrored: those of a symmetric matrix off its diagonal, which go to the other half as well.
+template <int T, int MODE>
+__device__ __forceinline__ void muon_results(const MuonArgs& a, const MuonOf& of, const MuonParts& parts, u64 row0, u64 col0, bool mirrored, f32x16_t (&sum)[T][T]) {
+  u8* const at = of.at;
+  const u32 r = of.r, c = of.c, lane = threadIdx.x & 63u, half = lane >> 5, in32 = lane & 31u;
+  const u32 planes = a.planes, which = a.which;
+  const int copy_type = a.copy_type;
+  const float keep = a.keep;
+  const bool turned = MODE >= kMuonFinish && a.t[of.i].turned;
+  void *const params = MODE >= kMuonFinish ? a.t[of.i].param : nullptr, *const copy = MODE >= kMuonFinish ? a.t[of.i].copy : nullptr;
+  const float step = MODE >= kMuonFinish ? -a.t[of.i].step * (1.0f / (kMuonScale * kMuonScale)) : 0.0f;
+  if (MODE >= kMuonFinish && a.grad_scale && !(fabsf(*a.grad_scale) < __builtin_inff())) return;
+  constexpr bool OF_X = MODE != kMuonGram && MODE != kMuonPoly;
+  const u64 along = OF_X ? parts.row_x : parts.row_t, cols = OF_X ? c : r;
+  // How many rows and columns there are from the wave's first on (what exceeds a tile does not matter), and values of a row with the zeros behind it.
+  const i32 rows_left = i32(min(i64(r) - i64(row0), i64(1024))), cols_left = i32(min(i64(cols) - i64(col0), i64(1024))), along_left = i32(min(i64(along) - i64(col0), i64(1024)));
+  // Rows of 32 x 32 one after the other: what is there already is asked for first, for the whole row.  WHOLE: the matrix has all of the wave's results.
+  const auto row_of_blocks = [&](auto number, auto whole) __attribute__((always_inline)) {
+    constexpr int i = decltype(number)::value;
+    constexpr bool WHOLE = decltype(whole)::value;
+#pragma unroll
+    for (int j = 0; j < T; ++j) muon_hold<T * T>(sum[i][j]);
+    const bool row_there = WHOLE || 32 * i + i32(in32) < rows_left;
+    if constexpr (MODE >= kMuonFinish) {
+      using One = typename ValueOf<MODE - kMuonFinish>::One;
+      constexpr bool WIDE = MODE == kMuonFinish + ZC_F32;
+      One* const param = static_cast<One*>(params);
+      // (Two blocks at a time: registers are short.)
+      constexpr int TOGETHER = T < 2 ? T : 2;
+#pragma unroll
+      for (int j0 = 0; j0 < T; j0 += TOGETHER) {
+        if (turned) {
+          const u64 first = (col0 + 16 * half) * r + row0 + 32 * i + in32;
+          One old[TOGETHER][16];
+#pragma unroll
+          for (int d = 0; d < TOGETHER; ++d)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const int at_col = 32 * (j0 + d) + k;
+              old[d][k] = j0 + d < T && row_there && (WHOLE || at_col + 16 * i32(half) < cols_left) ? param[first + u64(at_col) * r] : One(0.0f);
+            }
+#pragma unroll
+          for (int d = 0; d < TOGETHER; ++d)
+            if (j0 + d < T) {
+#pragma unroll
+              for (int k = 0; k < 16; ++k) {
+                const int at_col = 32 * (j0 + d) + k;
+                const float p = __builtin_fmaf(step, sum[i][j0 + d < T ? j0 + d : 0][k], float(old[d][k]) * keep);
+                if (row_there && (WHOLE || at_col + 16 * i32(half) < cols_left)) {
+                  param[first + u64(at_col) * r] = One(p);
+                  if (copy) store_value(copy, copy_type, first + u64(at_col) * r, p);
+                }
+              }
+            }
+        } else {
+          const u64 first = (row0 + 32 * i + in32) * c + col0 + 16 * half;
+          RawEight<WIDE> old[TOGETHER][2];
+          const auto left_of_piece = [&](int j, int h) { return WHOLE ? 8 : row_there && j < T ? cols_left - 32 * j - 16 * i32(half) - 8 * h : 0; };
+#pragma unroll
+          for (int d = 0; d < TOGETHER; ++d)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (j0 + d < T) old[d][h] = load_eight<WIDE>(param, first + 32 * (j0 + d) + 8 * h, left_of_piece(j0 + d, h));
+#pragma unroll
+          for (int d = 0; d < TOGETHER; ++d)
+            if (j0 + d < T) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float p[8];
+                numbers_of<WIDE>(old[d][h], MODE - kMuonFinish, p);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) p[k] = __builtin_fmaf(step, sum[i][j0 + d < T ? j0 + d : 0][8 * h + k], p[k] * keep);
+                store_eight<WIDE>(param, MODE - kMuonFinish, first + 32 * (j0 + d) + 8 * h, left_of_piece(j0 + d, h), p);
+                if (copy) store_numbers(copy, copy_type, first + 32 * (j0 + d) + 8 * h, left_of_piece(j0 + d, h), p);
+              }
+            }
+        }
+      }
+    } else {
+      // As it is, and turned: into the other half of a symmetric matrix (of a tile on the diagonal that is there already), or into the X turned that the next product reads.
+      // (Values behind the matrix's rows and columns are zeros, there and in the workspace, whose rows go on to a multiple of 128.)
+      const u64 to = uniform64((MODE == kMuonGram ? parts.a : MODE == kMuonPoly ? parts.b : parts.x) + 2 * ((row0 + 32 * i) * along + col0));
+      const u64 turned_to = uniform64((MODE == kMuonGram ? parts.a : MODE == kMuonPoly ? parts.b : which ? parts.t0 : parts.t1) + 2 * (col0 * parts.row_t + row0 + 32 * i));
+      const u32 mine = 2 * ((lane & 15u) * u32(along) + 8 * (lane >> 4)), mine_turned = 2 * ((16 * half + (lane & 3u)) * u32(parts.row_t) + (in32 & ~3u));
+      const auto there = [&](int j, int q) { return WHOLE || (32 * i + 16 * q + i32(lane & 15u) < rows_left && 32 * j + 8 * i32(lane >> 4) < along_left); };
+      const auto there_turned = [&](int j, int m) { return WHOLE || (32 * i + i32(in32 & ~3u) < rows_left && 32 * j + 16 * i32(half) + 4 * m + i32(lane & 3u) < cols_left); };
+      const u64 plane_to = OF_X ? parts.plane_x : parts.plane_a, plane_turned = OF_X ? parts.plane_t : parts.plane_a;
+      u32 old[MODE == kMuonPoly ? T : 1][2][8];
+      if constexpr (MODE == kMuonPoly) {
+        const u8* const from = at + uniform64(parts.a + 2 * ((row0 + 32 * i) * along + col0));
+#pragma unroll
+        for (u32 plane = 0; plane < 2; ++plane)
+          if (plane < planes) {
+#pragma unroll
+            for (int j = 0; j < T; ++j)
+#pragma unroll
+              for (int q = 0; q < 2; ++q) {
+                const u32x4_t p = there(j, q) ? *reinterpret_cast<const u32x4_t*>(at_bytes(from + plane * parts.plane_a + 32 * q * along + 64 * j, mine)) : u32x4_t{};
+#pragma unroll
+                for (int d = 0; d < 4; ++d) old[j][plane][4 * q + d] = p[d];
+              }
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < T; ++j) {
+        float v[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = sum[i][j][k] * (MODE == kMuonPoly ? kMuonC / kMuonScale : 1.0f / kMuonScale);
+        if constexpr (MODE == kMuonPoly) {
+#pragma unroll
+          for (u32 plane = 0; plane < 2; ++plane)
+            if (plane < planes) {
+              sixteen_to_memory(old[j][plane]);      // (the same exchange takes them back)
+#pragma unroll
+              for (int k = 0; k < 16; ++k) v[k] = __builtin_fmaf(half_of(old[j][plane], k), kMuonB, v[k]);
+            }
+          if (row0 + 32 * i == col0 + 32 * j) {       // (on the diagonal)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] += in32 == 16 * half + k ? kMuonA * kMuonScale : 0.0f;
+          }
+        }
+        const auto write = [&](u32 (&w)[8], u64 plane, u64 plane_t) __attribute__((always_inline)) {
+          if (MODE == kMuonUpdate || mirrored) {
+            const MuonTurn turn(lane);
+            u8* const base = at + turned_to + plane_t;
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+              const u32x2_t four = turn(w[2 * m], w[2 * m + 1]);
+              if (there_turned(j, m)) *reinterpret_cast<u32x2_t*>(at_bytes(base + 2 * (32 * j + 4 * m) * parts.row_t, mine_turned)) = four;
+            }
+          }
+          sixteen_to_memory(w);
+          u8* const base = at + to + plane;
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+            if (there(j, q)) *reinterpret_cast<u32x4_t*>(at_bytes(base + 32 * q * along + 64 * j, mine)) = u32x4_t{w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]};
+        };
+        u32 w[8];
+#pragma unroll
+        for (int d = 0; d < 8; ++d) w[d] = word_of_two<_Float16>(v[2 * d], v[2 * d + 1]);
+        if (planes > 1) {
+          u32 low[8];
+#pragma unroll
+          for (int d = 0; d < 8; ++d) low[d] = word_of_two<_Float16>(v[2 * d] - half_of(w, 2 * d), v[2 * d + 1] - half_of(w, 2 * d + 1));
+          write(low, plane_to, plane_turned);
+        }
+        write(w, 0, 0);
       }
     }
-  }
+  };
+  const auto all_rows = [&](auto whole) __attribute__((always_inline)) {
+    [&]<int... N>(std::integer_sequence<int, N...>) { (row_of_blocks(std::integral_constant<int, N>(), whole), ...); }(std::make_integer_sequence<int, T>());
+  };
+  if (rows_left >= 32 * T && cols_left >= 32 * T) all_rows(std::true_type());
+  else all_rows(std::false_type());
 }
 
 // Waits for all but the last N requests (they come back in the order in which they were made), for LDS, and for the workgroup's other waves.
@@ -342,10 +512,11 @@ constexpr u32 muon_lds_bytes(int T, int KB, int S) { return u32(S) * 2 * 64 * T 
 constexpr int muon_groups(int T, int KB, int S) { return T >= 3 ? 1 : int(163840u / muon_lds_bytes(T, KB, S)) < (T == 2 ? 2 : 4) ? int(163840u / muon_lds_bytes(T, KB, S)) : T == 2 ? 2 : 4; }
 
 template <int T, int KB, int S, int MODE>
-__global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : muon_groups(T, KB, S)) void muon_product_kernel(MuonArgs a) {
+__global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : muon_groups(T, KB, S)) void muon_product_kernel(MuonArgs) {
+  const MuonArgs& a = kernel_args<MuonArgs, 0>();
   constexpr u32 R = 64u * T, BLOCKS = KB / 8, ROW = 2 * KB, PLANE = R * ROW, STAGE = 2 * PLANE;      // bytes of a row, of an operand's rows, of a stage
   constexpr u32 APART = 4096 / ROW, LOADS = STAGE / 4096, STEPS = KB / 16;                           // rows between a thread's loads
-  static_assert(KB == 64 || KB == 32);
+  static_assert(KB == 64 || KB == 128);
   __shared__ u32x4_t memory[S * STAGE / 16];
   const u32 tid = threadIdx.x, lane = tid & 63u, wave = uniform(tid >> 6), half = lane >> 5, in32 = lane & 31u;
   const MuonTiles<MODE> tiles(a.count);
@@ -353,27 +524,33 @@ __global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : m
 
   // What is asked for next: a tile's rows, and how far along them.
   u32 ask_tile = tiles.first, ask_stage = 0, ask_stages = 0, ask_segment = 0;
-  u32 ask_stride = 0;
   MuonRows rows_a, rows_b;
   const u32 my_row = tid / BLOCKS;
   // Which block of a row is where: the place's number exchanged by what tells the rows apart that are read together.
-  const auto key_a = [](u32 row) { return KB == 64 ? row >> 1 & 7u : row >> 2 & 3u; };
-  const auto key_b = [](u32 row) { return KB == 64 ? (row >> 1 & 1u) | (row >> 3 & 2u) | (row & 4u) : (row >> 2 & 1u) | (row >> 3 & 2u); };
-  const u32 block_a = 16u * ((tid ^ key_a(my_row)) & (BLOCKS - 1)), block_b = 16u * ((tid ^ key_b(my_row)) & (BLOCKS - 1));
+  const auto key_a = [](u32 row) { return KB == 128 ? row & 15u : row >> 1 & 7u; };
+  const auto key_b = [](u32 row) { return KB == 128 ? (row & 7u) | (row >> 1 & 8u) : (row >> 1 & 1u) | (row >> 3 & 2u) | (row & 4u); };
+  u32 mine_a[LOADS / 2], mine_b[LOADS / 2];          // a thread's places in the tile's rows
   const auto aim = [&] {
-    const u32 i = muon_tensor_of(a, ask_tile), r = a.t[i].r, c = a.t[i].c;
+    const MuonOf of(a, ask_tile);
+    const u32 r = of.r, c = of.c;
     const MuonParts parts(r, c, a.planes);
     u32 row, col;
     const u32 down = (r + R - 1) / R, across = MODE == kMuonGram || MODE == kMuonPoly ? down : (c + R - 1) / R;
-    MuonTiles<MODE>::place(ask_tile - a.first[i], down, across, row, col);
-    const u8* const at = a.t[i].at;
+    MuonTiles<MODE>::place(ask_tile - of.first, down, across, row, col);
+    const u8* const at = of.at;
     const u64 plane_a = MODE == kMuonGram ? parts.plane_x : parts.plane_a, plane_b = MODE == kMuonGram ? parts.plane_x : MODE == kMuonPoly ? parts.plane_a : parts.plane_t;
     const u8* const from_a = at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : parts.b) + (ask_segment == 2 ? plane_a : 0);
     const u8* const from_b = at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : a.which ? parts.t1 : parts.t0) + (ask_segment == 1 ? plane_b : 0);
     const u64 along = MODE == kMuonGram ? parts.row_x : parts.row_t;
     rows_a.aim(from_a, u64(row) * R, r, 2 * along, R);
     rows_b.aim(from_b, u64(col) * R, MODE == kMuonGram || MODE == kMuonPoly ? r : c, 2 * along, R);
-    ask_stride = uniform(u32(2 * along));
+    const u32 apart = uniform(u32(2 * along));
+#pragma unroll
+    for (u32 k = 0; k < LOADS / 2; ++k) {
+      const u32 of = my_row + APART * k;
+      mine_a[k] = of * apart + 16u * ((tid ^ key_a(of)) & (BLOCKS - 1));
+      mine_b[k] = of * apart + 16u * ((tid ^ key_b(of)) & (BLOCKS - 1));
+    }
     ask_stages = uniform(u32(along / KB));
   };
   // (Behind the last tile there is nothing to ask for.)
@@ -394,15 +571,16 @@ __global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : m
   const u32 lds0 = u32(reinterpret_cast<uintptr_t>((LdsWord*)&memory[0]));
   const auto ask = [&](u32 place, u32 i) {           // place: of the stage in LDS, in bytes
     const u32 to = lds0 + wave * 1024u + place + 4096u * i;
-    if (i < LOADS / 2) muon_load_to_lds(rows_a.buffer(), to, (my_row + APART * i) * ask_stride + block_a);
-    else muon_load_to_lds(rows_b.buffer(), to, (my_row + APART * (i - LOADS / 2)) * ask_stride + block_b);
+    if (i < LOADS / 2) muon_load_to_lds(rows_a.buffer(), to, mine_a[i]);
+    else muon_load_to_lds(rows_b.buffer(), to, mine_b[i - LOADS / 2]);
   };
 
   const u32 wave_a = (wave >> 1) * 32u * T, wave_b = (wave & 1u) * 32u * T;
   const u32 lane_b = (in32 & 3u) + 16u * ((in32 >> 2) & 1u) + 4u * (in32 >> 3);
-  // The blocks of this step and of the next one; in tiles of 64, where a step is one instruction, less than LDS takes to answer, those of this stage and of the next one.
-  constexpr u32 AHEAD = T == 1 ? STEPS : 1;
-  u32x4_t fa[2 * AHEAD][T], fb[2 * AHEAD][T];
+  // The blocks of this step and of the next two (one, where registers are short); in tiles of 64, where a step is one instruction, less than LDS takes to answer, those of this stage and of the next one.
+  constexpr u32 AHEAD = T == 1 ? STEPS : T == 4 || (T == 3 && MODE == kMuonPoly) ? 1 : 2, HELD = T == 1 ? 2 * STEPS : STEPS;
+  static_assert(STEPS == 4 || T == 1);
+  u32x4_t fa[HELD][T], fb[HELD][T];
   u32 at_a[STEPS], at_b[STEPS];                      // where a lane's block of step t is, in the first stage's place
 #pragma unroll
   for (u32 t = 0; t < STEPS; ++t) {
@@ -415,28 +593,32 @@ __global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : m
     else fb[to][i - T] = *reinterpret_cast<LdsBlock*>(at_b[t] + place + 32 * ROW * (i - T));
   };
 
-  // The instructions of a step and what goes between them: in the first half the reads for the next step; in the last step of a stage, once everybody has read that stage,
-  // half of the requests for the stage that takes its place, and the other half in the step behind it.
+  // The instructions of a step and what goes between them: in the first half the reads for the steps to come; once everybody has read a stage, half of the requests for the one that takes
+  // its place, and the other half in the step behind that.
   constexpr u32 SLOTS = T * T, READS = 2 * T, EARLY = LOADS / 2;
   aim();
   const auto behind = [](u32 place) { return place + STAGE == S * STAGE ? 0u : place + STAGE; };
   u32 now = 0, free = 0;                             // the stage that is multiplied; the one that is asked for
+  constexpr int FIRST = T == 1 || AHEAD == 1 ? S - 1 : S;    // stages that are asked for before the first one is multiplied
 #pragma unroll
-  for (int s = 0; s + 1 < S; ++s) {
+  for (int s = 0; s < FIRST; ++s) {
 #pragma unroll
     for (u32 i = 0; i < LOADS; ++i) ask(free, i);
     next_stage();
     free = behind(free);
   }
-  muon_wait<(S - 2) * int(LOADS)>();
+  muon_wait<(FIRST - 1) * int(LOADS)>();
+  if constexpr (T == 1 || AHEAD == 1) {
 #pragma unroll
-  for (u32 i = 0; i < EARLY; ++i) ask(free, i);
+    for (u32 i = 0; i < EARLY; ++i) ask(free, i);
+  }
 #pragma unroll
   for (u32 t = 0; t < AHEAD; ++t)
 #pragma unroll
     for (u32 i = 0; i < READS; ++i) read(t, 0, t, i);
   for (u32 tile = tiles.first; tile < tiles.end; tile += tiles.step) {
-    const u32 ti = muon_tensor_of(a, tile), r = a.t[ti].r, c = a.t[ti].c;
+    const MuonOf of(a, tile);
+    const u32 r = of.r, c = of.c;
     const MuonParts parts(r, c, a.planes);
     const u32 stages = uniform(u32((MODE == kMuonGram ? parts.row_x : parts.row_t) / KB) * (a.planes > 1 ? 3u : 1u));
     f32x16_t sum[T][T];
@@ -449,7 +631,12 @@ __global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : m
     if constexpr (T == 1) {
       for (u32 pair = 0; pair < stages; pair += 2) {
 #pragma unroll
-        for (u32 u = 0; u < 2; ++u) {                  // (of an even number of stages)
+        for (u32 u = 0; u < 2; ++u) {
+          if (u && pair + 1 == stages) {               // an odd number of stages: what has been read for the next tile goes where that looks for it
+#pragma unroll
+            for (u32 t = 0; t < STEPS; ++t) fa[t][0] = fa[STEPS + t][0], fb[t][0] = fb[STEPS + t][0];
+            break;
+          }
           const u32 next = behind(now);
 #pragma unroll
           for (u32 i = 0; i < EARLY; ++i) ask(free, EARLY + i);
@@ -473,25 +660,27 @@ __global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : m
         const u32 next = behind(now);
 #pragma unroll
         for (u32 t = 0; t < STEPS; ++t) {
-          if (t == STEPS - 1) muon_wait<(S - 2) * int(LOADS)>();
+          if (t == STEPS - AHEAD) muon_wait<(S - 2) * int(LOADS)>();
 #pragma unroll
           for (u32 slot = 0; slot < SLOTS; ++slot) {
 #pragma unroll
             for (u32 i = 0; i < EARLY; ++i) {
               if (i * SLOTS / EARLY != slot) continue;
-              if (t == STEPS - 1) ask(now, i);
-              if (t == 0) ask(free, EARLY + i);
+              if (t == STEPS - AHEAD) ask(now, i);
+              if (AHEAD == 1 && t == 0) ask(free, EARLY + i);
+              if (AHEAD > 1 && t == STEPS - AHEAD + 1) ask(now, EARLY + i);
             }
 #pragma unroll
             for (u32 i = 0; i < READS; ++i)
-              if (i * SLOTS / (2 * READS) == slot) read((t + 1) & 1, t + 1 < STEPS ? now : next, (t + 1) % STEPS, i);
+              if (i * SLOTS / (2 * READS) == slot) read((t + AHEAD) % STEPS, t + AHEAD < STEPS ? now : next, (t + AHEAD) % STEPS, i);
             const u32 i = slot / T, j = slot % T;
-            sum[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, fb[t & 1][j]), __builtin_bit_cast(f16x8_t, fa[t & 1][i]), sum[i][j], 0, 0, 0);
+            sum[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, fb[t][j]), __builtin_bit_cast(f16x8_t, fa[t][i]), sum[i][j], 0, 0, 0);
             muon_hold<T * T>(sum[i][j]);
             __builtin_amdgcn_sched_barrier(0);
           }
-          if (t == 0) next_stage();
+          if (AHEAD == 1 && t == 0) next_stage();
         }
+        if (AHEAD > 1) next_stage();
         free = now;
         now = next;
       }
@@ -499,131 +688,97 @@ __global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : m
     // The results.
     u32 down, across;
     const u32 tiles_down = (r + R - 1) / R, tiles_across = MODE == kMuonGram || MODE == kMuonPoly ? tiles_down : (c + R - 1) / R;
-    MuonTiles<MODE>::place(tile - a.first[ti], tiles_down, tiles_across, down, across);
-    const u64 row0 = u64(down) * R + wave_a, col0 = u64(across) * R + wave_b;      // the wave's
-    u8* const at = a.t[ti].at;
-    if (MODE >= kMuonFinish && a.grad_scale && !(fabsf(*a.grad_scale) < __builtin_inff())) continue;
-    // Where a lane's results of 32 x 32 are.
-    constexpr bool OF_X = MODE != kMuonGram && MODE != kMuonPoly;
-    const u64 along = OF_X ? parts.row_x : parts.row_t;
-    const auto row_of = [&](int i) { return row0 + 32 * i + in32; };
-    const auto col_of = [&](int j) { return col0 + 32 * j + 16 * half; };
-    const auto place_of = [&](int i, int j) {
-      MuonPlace place;
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const u64 of_row = row0 + 32 * i + 16 * q + (lane & 15u), of_col = col0 + 32 * j + 8 * (lane >> 4);
-        place.at[q] = 2 * (of_row * along + of_col);
-        place.there[q] = of_row < r && of_col < along;
-      }
-      return place;
-    };
-    // Rows of 32 x 32 one after the other: what is there already is asked for first, for the whole row.
-    const auto row_of_blocks = [&](auto number) __attribute__((always_inline)) {
-      constexpr int i = decltype(number)::value;
-#pragma unroll
-      for (int j = 0; j < T; ++j) muon_hold<T * T>(sum[i][j]);
-      if constexpr (MODE >= kMuonFinish) {
-        using One = typename ValueOf<MODE - kMuonFinish>::One;
-        constexpr bool WIDE = MODE == kMuonFinish + ZC_F32;
-        One* const param = static_cast<One*>(a.t[ti].param);
-        void* const copy = a.t[ti].copy;
-        const float step = -a.t[ti].step * (1.0f / (kMuonScale * kMuonScale));
-        const u64 row = row_of(i);
-        if (a.t[ti].turned) {
-          One old[T][16];
-#pragma unroll
-          for (int j = 0; j < T; ++j)
-#pragma unroll
-            for (int k = 0; k < 16; ++k) old[j][k] = row < r && col_of(j) + k < c ? param[(col_of(j) + k) * r + row] : One(0.0f);
-#pragma unroll
-          for (int j = 0; j < T; ++j)
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float p = __builtin_fmaf(step, sum[i][j][k], float(old[j][k]) * a.keep);
-              const u64 place = (col_of(j) + k) * r + row;
-              if (row < r && col_of(j) + k < c) {
-                param[place] = One(p);
-                if (copy) store_value(copy, a.copy_type, place, p);
-              }
-            }
-        } else {
-          RawEight<WIDE> old[T][2];
-          i32 left[T];
-#pragma unroll
-          for (int j = 0; j < T; ++j) {
-            left[j] = row < r && col_of(j) < c ? i32(min(c - col_of(j), u64(16))) : 0;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) old[j][h] = load_eight<WIDE>(param, row * c + col_of(j) + 8 * h, left[j] - 8 * h);
-          }
-#pragma unroll
-          for (int j = 0; j < T; ++j)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              float p[8];
-              const u64 place = row * c + col_of(j) + 8 * h;
-              numbers_of<WIDE>(old[j][h], MODE - kMuonFinish, p);
-#pragma unroll
-              for (int k = 0; k < 8; ++k) p[k] = __builtin_fmaf(step, sum[i][j][8 * h + k], p[k] * a.keep);
-              store_eight<WIDE>(param, MODE - kMuonFinish, place, left[j] - 8 * h, p);
-              if (copy) store_numbers(copy, a.copy_type, place, left[j] - 8 * h, p);
-            }
-        }
-      } else {
-        // As it is, and turned: into the other half of a symmetric matrix (of a tile on the diagonal that is there already), or into the X turned that the next product reads.
-        // (Values behind the matrix's columns are zeros, there and in the workspace, whose rows go on to a multiple of 128.)
-        u8* const to = at + (MODE == kMuonGram ? parts.a : MODE == kMuonPoly ? parts.b : parts.x);
-        u8* const other = at + (MODE == kMuonGram ? parts.a : MODE == kMuonPoly ? parts.b : a.which ? parts.t0 : parts.t1);
-        const u64 row4 = row0 + 32 * i + (in32 & ~3u);
-        const i32 rows4 = row4 < r ? i32(min(r - row4, u64(4))) : 0;
-        u32 old[MODE == kMuonPoly ? T : 1][2][8];
-        if constexpr (MODE == kMuonPoly) {
-#pragma unroll
-          for (int j = 0; j < T; ++j) {
-            read_sixteen(at + parts.a, place_of(i, j), old[j][0]);
-            if (a.planes > 1) read_sixteen(at + parts.a + parts.plane_a, place_of(i, j), old[j][1]);
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < T; ++j) {
-          const u64 col4 = col_of(j) + (lane & 3u);
-          const i32 left4 = col_of(j) < (OF_X ? c : r) ? i32(min((OF_X ? c : r) - col_of(j), u64(16))) : 0;
-          const MuonPlace place = place_of(i, j);
-          float v[16];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) v[k] = sum[i][j][k] * (MODE == kMuonPoly ? kMuonC / kMuonScale : 1.0f / kMuonScale);
-          if constexpr (MODE == kMuonPoly) {
-            sixteen_to_memory(old[j][0]);              // (the same exchange takes them back)
-            if (a.planes > 1) sixteen_to_memory(old[j][1]);
-            const i32 diagonal = i32(min(i64(row_of(i)) - i64(col_of(j)) + 64, i64(127))) - 64;
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              float x = half_of(old[j][0], k);
-              if (a.planes > 1) x += half_of(old[j][1], k);
-              v[k] = __builtin_fmaf(x, kMuonB, v[k]);
-              if (k == diagonal) v[k] += kMuonA * kMuonScale;
-            }
-          }
-          const auto both = [&](u32 (&w)[8], u64 plane, u64 plane_turned) __attribute__((always_inline)) {
-            if (MODE == kMuonUpdate || down != across) write_turned(other + plane_turned + 2 * (col4 * parts.row_t + row4), parts.row_t, rows4, left4, lane, w);
-            write_sixteen(to + plane, place, w);
-          };
-          u32 w[8];
-#pragma unroll
-          for (int d = 0; d < 8; ++d) w[d] = word_of_two<_Float16>(v[2 * d], v[2 * d + 1]);
-          if (a.planes > 1) {
-            u32 low[8];
-#pragma unroll
-            for (int d = 0; d < 8; ++d) low[d] = word_of_two<_Float16>(v[2 * d] - half_of(w, 2 * d), v[2 * d + 1] - half_of(w, 2 * d + 1));
-            both(low, MODE == kMuonUpdate ? parts.plane_x : parts.plane_a, MODE == kMuonUpdate ? parts.plane_t : parts.plane_a);
-          }
-          both(w, 0, 0);
-        }
-      }
-    };
-    [&]<int... N>(std::integer_sequence<int, N...>) { (row_of_blocks(std::integral_constant<int, N>()), ...); }(std::make_integer_sequence<int, T>());
+    MuonTiles<MODE>::place(tile - of.first, tiles_down, tiles_across, down, across);
+    muon_results<T, MODE>(a, of, parts, u64(down) * R + wave_a, u64(across) * R + wave_b, down != across, sum);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (the last requests, too, before the workgroup's LDS is given to another one)
+}
+
+// ---- Few and small results: workgroups make tiles of 32 x 32, and their four waves take every fourth stage of 64 values each, by themselves: a wave's requests go to a part of LDS of its own, and
+// it waits for nobody.  At the end the first wave adds the four sums.  (Tiles of 64 of the sizes for which this is there are bound by what a workgroup waits for itself: three matrices of
+// 333 x 1531 in two parts, 63 tiles on 256 CUs, 21 us for X X^T, 0.25 us a stage.)
+template <int S, int MODE>
+__global__ __launch_bounds__(256, S == 2 ? 2 : 1) void muon_small_kernel(MuonArgs) {
+  const MuonArgs& a = kernel_args<MuonArgs, 0>();
+  constexpr u32 STAGE = 8192;                        // of a wave: 32 rows of each operand
+  __shared__ u32x4_t memory[4 * S * STAGE / 16];
+  const u32 lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), half = lane >> 5, in32 = lane & 31u;
+  const MuonTiles<MODE> tiles(a.count);
+  const MuonOf of(a, tiles.first);                   // (a workgroup has one tile)
+  const u32 r = of.r, c = of.c;
+  const MuonParts parts(r, c, a.planes);
+  u32 down, across;
+  constexpr bool TRIANGLE = MODE == kMuonGram || MODE == kMuonPoly;
+  const u32 tiles_down = (r + 31) / 32, tiles_across = TRIANGLE ? tiles_down : (c + 31) / 32;
+  MuonTiles<MODE>::place(tiles.first - of.first, tiles_down, tiles_across, down, across);
+  const u64 along = MODE == kMuonGram ? parts.row_x : parts.row_t;
+  const u32 per = u32(along / 64), stages = per * (a.planes > 1 ? 3u : 1u), apart = u32(2 * along);
+  const u64 plane_a = MODE == kMuonGram ? parts.plane_x : parts.plane_a, plane_b = MODE == kMuonGram ? parts.plane_x : MODE == kMuonPoly ? parts.plane_a : parts.plane_t;
+  const u8* const of_a = of.at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : parts.b);
+  const u8* const of_b = of.at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : a.which ? parts.t1 : parts.t0);
+  const auto key_a = [](u32 row) { return row >> 1 & 7u; };
+  const auto key_b = [](u32 row) { return (row >> 1 & 1u) | (row >> 3 & 2u) | (row & 4u); };
+  u32 mine_a[4], mine_b[4];
+#pragma unroll
+  for (u32 k = 0; k < 4; ++k) {
+    const u32 row = (lane >> 3) + 8 * k;
+    mine_a[k] = row * apart + 16u * ((lane ^ key_a(row)) & 7u);
+    mine_b[k] = row * apart + 16u * ((lane ^ key_b(row)) & 7u);
+  }
+  const u32 lds0 = u32(reinterpret_cast<uintptr_t>((LdsWord*)&memory[0])) + wave * S * STAGE;
+  u32 ask_segment = 0, ask_at = wave, asked = wave;  // the stage that is asked for next, in its product of parts and in all
+  const auto ask = [&](u32 place) {
+    while (ask_at >= per) ask_at -= per, ++ask_segment;
+    MuonRows rows_a, rows_b;
+    rows_a.aim(of_a + (ask_segment == 2 ? plane_a : 0), u64(down) * 32, r, apart, 32);
+    rows_b.aim(of_b + (ask_segment == 1 ? plane_b : 0), u64(across) * 32, TRIANGLE ? r : c, apart, 32);
+    rows_a.move_on(128 * ask_at);
+    rows_b.move_on(128 * ask_at);
+    if (asked >= stages) rows_a.bytes = rows_b.bytes = 0;      // (behind the last stage there is nothing to ask for)
+#pragma unroll
+    for (u32 k = 0; k < 4; ++k) muon_load_to_lds(rows_a.buffer(), lds0 + place + 1024u * k, mine_a[k]);
+#pragma unroll
+    for (u32 k = 0; k < 4; ++k) muon_load_to_lds(rows_b.buffer(), lds0 + place + 4096u + 1024u * k, mine_b[k]);
+    ask_at += 4;
+    asked += 4;
+  };
+  const u32 lane_b = (in32 & 3u) + 16u * ((in32 >> 2) & 1u) + 4u * (in32 >> 3);
+  typedef const __attribute__((address_space(3))) u32x4_t LdsBlock;
+  f32x16_t sum[1][1] = {}, other = {};
+  u32 now = 0, free = 0;
+  const auto behind = [](u32 place) { return place + STAGE == S * STAGE ? 0u : place + STAGE; };
+#pragma unroll
+  for (int s = 0; s + 1 < S; ++s) ask(free), free = behind(free);
+  for (u32 stage = wave; stage < stages; stage += 4) {
+    ask(free);
+    free = behind(free);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 1) * 8) : "memory");
+    f16x8_t x[4], y[4];
+#pragma unroll
+    for (u32 t = 0; t < 4; ++t) {
+      x[t] = __builtin_bit_cast(f16x8_t, *reinterpret_cast<LdsBlock*>(lds0 + now + in32 * 128u + 16u * ((4 * half + t) ^ key_a(in32))));
+      y[t] = __builtin_bit_cast(f16x8_t, *reinterpret_cast<LdsBlock*>(lds0 + now + 4096u + lane_b * 128u + 16u * ((4 * half + t) ^ key_b(lane_b))));
+    }
+    now = behind(now);
+#pragma unroll
+    for (u32 t = 0; t < 4; t += 2) {
+      sum[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(y[t], x[t], sum[0][0], 0, 0, 0);
+      other = __builtin_amdgcn_mfma_f32_32x32x16_f16(y[t + 1], x[t + 1], other, 0, 0, 0);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // (what has been read may be overwritten)
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  float* const sums = reinterpret_cast<float*>(&memory[0]);   // [wave][value][lane]
+  if (wave) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sums[(wave * 16 + k) * 64 + lane] = sum[0][0][k] + other[k];
+  }
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) sum[0][0][k] = ((sum[0][0][k] + other[k]) + sums[(16 + k) * 64 + lane]) + (sums[(32 + k) * 64 + lane] + sums[(48 + k) * 64 + lane]);
+  muon_results<1, MODE>(a, of, parts, u64(down) * 32, u64(across) * 32, down != across, sum);
 }
 
 }  // namespace zc

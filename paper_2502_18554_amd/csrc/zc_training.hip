@@ -128,41 +128,61 @@ u64 muon_tiles(const MuonTensor& t, int mode, u64 side) {
   const u64 down = (t.r + side - 1) / side, across = (t.c + side - 1) / side;
   return mode == kMuonGram || mode == kMuonPoly ? down * (down + 1) / 2 : down * across;
 }
-constexpr int muon_stages(int T) { return T == 4 ? 2 : T == 3 ? 3 : T == 2 ? 2 : 4; }        // that lie in LDS
-template <int T, int MODE>
-void launch_muon_product(MuonArgs& a, hipStream_t stream) {
+// Calls of tiles of `side`, in ascending order of the matrices.
+template <int MODE>
+void count_muon_tiles(MuonArgs& a, u64 side) {
   a.count = 0;
   for (u32 i = 0; i < a.tensors; ++i) {
     a.first[i] = a.count;
-    a.count += u32(muon_tiles(a.t[i], MODE, 64 * T));
+    a.count += u32(muon_tiles(a.t[i], MODE, side));
   }
+  if (a.each) a.each = a.count / a.tensors;
+}
+constexpr int muon_stages(int T) { return T == 3 ? 3 : T == 1 ? 4 : 2; }        // that lie in LDS
+template <int T, int MODE>
+void launch_muon_tiles(MuonArgs& a, hipStream_t stream) {
+  count_muon_tiles<MODE>(a, 64 * T);
   const u32 at_once = 256 * muon_groups(T, 64, muon_stages(T));
   hipLaunchKernelGGL((muon_product_kernel<T, 64, muon_stages(T), MODE>), dim3(a.count < at_once ? a.count : at_once), dim3(256), 0, stream, a);
 }
 // The size of tile that takes the least time, in us, by what a turn of all CUs has been measured to take: a tile's begin and end, and its stages of 64 values.
+// (X X^T of three matrices of 333 x 1531 in two parts: tiles of 32, 64 and 128 9.5, 21 and 33 us; 24 of 256 x 512: 8.4, 6.9 and 9.1; six of 1024 x 4096 in two parts, tiles of 64, 128, 192 and 256:
+// 146, 120, 141 and 223; 4096 x 8192, tiles of 128, 192 and 256: 181, 123 and 154.)
 template <int MODE>
 void launch_muon_product(MuonArgs& a, hipStream_t stream) {
-  double tiles[4] = {}, along[4] = {};
+  constexpr int SIDES = 5;
+  constexpr u64 sides[SIDES] = {32, 64, 128, 192, 256};
+  double tiles[SIDES] = {}, along[SIDES] = {};
   for (u32 i = 0; i < a.tensors; ++i) {
     const double stages = double(muon_along(MODE == kMuonGram ? a.t[i].c : a.t[i].r)) / 64 * (a.planes > 1 ? 3 : 1);
-    for (int t = 0; t < 4; ++t) {
-      const double of_this = double(muon_tiles(a.t[i], MODE, u64(64) * (t + 1)));
+    for (int t = 0; t < SIDES; ++t) {
+      const double of_this = double(muon_tiles(a.t[i], MODE, sides[t]));
       tiles[t] += of_this;
       along[t] += of_this * stages;
     }
   }
   const auto stages = [&](int t) { return along[t] / tiles[t]; };
-  const double cost[4] = {3 + (tiles[0] <= 256 ? 2 + 0.25 * stages(0) : std::ceil(tiles[0] / 512) * (1.5 + 0.4 * stages(0))),
-                          tiles[1] <= 256 ? 9 + 0.6 * stages(1) : 4 + std::ceil(tiles[1] / 512) * (12 + 1.1 * stages(1)),
-                          std::ceil(tiles[2] / 256) * (12 + (tiles[2] <= 160 ? 0.68 : 0.85) * stages(2)),
-                          std::ceil(tiles[3] / 256) * (22 + (tiles[3] <= 160 ? 1.15 : 1.45) * stages(3))};
+  const auto turns = [&](int t, double at_once) { return std::ceil(tiles[t] / at_once); };
+  const double cost[SIDES] = {2 + turns(0, 512) * (2.3 + (tiles[0] <= 512 ? 0.075 : 0.16) * stages(0)),
+                              3 + (tiles[1] <= 256 ? 2 + 0.25 * stages(1) : turns(1, 512) * (3 + 0.5 * stages(1))),
+                              tiles[2] <= 256 ? 7 + 0.6 * stages(2) : 4 + turns(2, 512) * (12 + 1.1 * stages(2)),
+                              turns(3, 256) * (12 + (tiles[3] <= 160 ? 0.68 : 0.83) * stages(3)),
+                              turns(4, 256) * (22 + (tiles[4] <= 160 ? 1.1 : 1.4) * stages(4))};
   int best = 0;
-  for (int t = 1; t < 4; ++t)
+  for (int t = 1; t < (MODE == kMuonPoly ? SIDES - 1 : SIDES); ++t)            // (tiles of 256 have no registers left for what the second product reads as well)
     if (cost[t] < cost[best]) best = t;
-  if (best == 0) launch_muon_product<1, MODE>(a, stream);
-  else if (best == 1) launch_muon_product<2, MODE>(a, stream);
-  else if (best == 2) launch_muon_product<3, MODE>(a, stream);
-  else launch_muon_product<4, MODE>(a, stream);
+  if (best == 0) {
+    count_muon_tiles<MODE>(a, 32);
+    hipLaunchKernelGGL((muon_small_kernel<2, MODE>), dim3(a.count), dim3(256), 0, stream, a);
+  } else if (best == 1) {
+    launch_muon_tiles<1, MODE>(a, stream);
+  } else if (best == 2) {
+    launch_muon_tiles<2, MODE>(a, stream);
+  } else if (best == 3) {
+    launch_muon_tiles<3, MODE>(a, stream);
+  } else if constexpr (MODE != kMuonPoly) {
+    launch_muon_tiles<4, MODE>(a, stream);
+  }
 }
 
 // A launch of `groups(i)` workgroups for matrix i.
@@ -173,6 +193,7 @@ void launch_muon(K kernel, MuonArgs& a, const F& groups, hipStream_t stream) {
     a.first[i] = a.count;
     a.count += u32(groups(a.t[i]));
   }
+  if (a.each) a.each = a.count / a.tensors;
   if (a.count) hipLaunchKernelGGL(kernel, dim3(a.count), dim3(256), 0, stream, a);
 }
 
@@ -341,12 +362,17 @@ int zc_muon(int k, const size_t* rows, const size_t* cols, void* const* d_params
     }
     if (!a.tensors) continue;
     u8* at = static_cast<u8*>(d_ws) + u64(a.tensors) * kMuonPartials * 8;
-    bool padded = false;
+    bool padded = false, alike = true;
     for (u32 j = 0; j < a.tensors; ++j) {
       a.t[j].at = at;
       at += pad256(MuonParts(a.t[j].r, a.t[j].c, planes).bytes);
       padded |= a.t[j].r % kMuonAlong != 0;
+      alike &= a.t[j].r == a.t[0].r && a.t[j].c == a.t[0].c;
     }
+    a.r = a.t[0].r, a.c = a.t[0].c;
+    a.at = a.t[0].at;
+    a.bytes = pad256(MuonParts(a.r, a.c, planes).bytes);
+    a.each = alike ? 1 : 0;                              // (each launch puts its number here)
     launch_muon(muon_momentum_kernel, a, [](const MuonTensor& t) { return muon_partials(u64(t.r) * t.c); }, stream);
     launch_muon(muon_begin_kernel, a, [](const MuonTensor& t) { return muon_along(t.r) / 64 * (muon_along(t.c) / 64); }, stream);
     if (padded) launch_muon(muon_zeros_kernel, a, [](const MuonTensor& t) { return (t.c + 15) / 16; }, stream);

@@ -51,9 +51,9 @@ def off(got, want):
     return np.linalg.norm(got - want) / max(np.linalg.norm(want), 1e-30)
 
 
-def allowed(u, iterations, wide):
-    exact = model.orthogonalised(u, iterations, 0)
-    return 1.5 * off(model.orthogonalised(u, iterations, 2 if wide else 1), exact) + 2.0 ** -17
+def allowed(u, iterations, wide, device="cpu"):
+    exact = model.orthogonalised(u, iterations, 0, device)
+    return 1.5 * off(model.orthogonalised(u, iterations, 2 if wide else 1, device), exact) + 2.0 ** -17
 
 
 SHAPES = [(1, 1), (1, 7), (5, 3), (17, 17), (40, 30), (64, 64), (65, 130), (128, 128), (129, 257), (300, 100), (256, 512), (513, 700), (1100, 1300), (1290, 1030), (96, 4000)]
@@ -70,6 +70,26 @@ def test_directions(rows, cols, wide):
     want, m = model.muon(np.zeros((rows, cols)), values(grad), np.zeros((rows, cols)), 1.0, 0.0, 0.0, 5, False)
     assert off(values(p), want) <= allowed(values(grad), 5, wide)
     assert np.array_equal(values(parts_of(state, [(rows, cols)])[0]), values(grad))
+
+
+# (rows, columns, matrices): between them, each of the three products goes by tiles of 32, 64, 128, 192 and 256 (the second one not by 256), whole and cut ones, several to a workgroup
+LARGE = [(256, 512, 24, False), (333, 1531, 3, True), (700, 2100, 2, True), (1000, 1900, 6, False), (1024, 4096, 6, True), (2100, 3000, 1, False), (2050, 4100, 2, False), (4000, 4100, 1, False), (1536, 1536, 5, True),
+         (4500, 2300, 3, False)]
+
+
+@pytest.mark.parametrize("rows,cols,count,wide", LARGE)
+def test_directions_of_larger_matrices(rows, cols, count, wide):
+    """The same in 64 bits on the GPU; matrices of one shape, and with one of another among them."""
+    g = generator(rows + 7 * cols)
+    for more in ([], [(70, 200)]):
+        shapes = [(rows, cols)] * count + more
+        grads = [gradient(*s, g) for s in shapes]
+        p = [torch.zeros(s, device=DEV) for s in shapes]
+        assert zc.zc_muon(p, grads, state_of(shapes), workspace(shapes, wide), 1.0, momentum=0.0, nesterov=False, wide=wide) == 0
+        for i in {0, count - 1, len(shapes) - 1}:
+            r, c = shapes[i]
+            want = -model.orthogonalised(values(grads[i]), 5, 0, DEV) * max(1, r / c) ** 0.5
+            assert off(values(p[i]), want) <= allowed(values(grads[i]), 5, wide, DEV)
 
 
 @pytest.mark.parametrize("kinds", [("f32", "f32", None), ("f32", "bf16", "bf16"), ("bf16", "f16", None), ("f16", "bf16", "f32")])

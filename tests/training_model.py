@@ -1,5 +1,6 @@
-"""Layer norm, embedding and the step for matrices from their definitions, in numpy and in 64 bits: what the calls are compared with."""
+"""Layer norm, embedding and the step for matrices from their definitions, in 64 bits: what the calls are compared with."""
 import numpy as np
+import torch
 
 U = 2.0 ** -24                               # half a step of binary32 relative to the value
 HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
@@ -53,25 +54,25 @@ SCALE = 4096.0
 
 def rounded(x, parts):
     """To one binary16 number, or to the sum of two, at the scale that the kernels keep."""
-    y = x * SCALE
-    high = y.astype(np.float16).astype(np.float64)
     if parts == 0:
         return x
-    return (high if parts == 1 else high + (y - high).astype(np.float16).astype(np.float64)) / SCALE
+    y = x * SCALE
+    high = y.half().double()
+    return (high if parts == 1 else high + (y - high).half().double()) / SCALE
 
 
-def orthogonalised(u, iterations, parts):
+def orthogonalised(u, iterations, parts, device="cpu"):
     """X after so many iterations; parts 0: nothing rounded, 1 and 2: operands rounded to one and two binary16 numbers, as the kernels round them."""
     turned = u.shape[0] > u.shape[1]
-    x = u.T if turned else u
-    x = rounded(x / max(np.sqrt((x * x).sum()), 1e-7), parts)
+    x = torch.from_numpy(np.ascontiguousarray(u.T if turned else u)).double().to(device)
+    x = rounded(x / max(float(x.square().sum().sqrt()), 1e-7), parts)
     for i in range(iterations):
-        a = rounded(x @ x.T, parts)
-        b = rounded(A * np.eye(len(a)) + B * a + C * (a @ a), parts)
+        a = rounded(x @ x.t().contiguous(), parts)
+        b = rounded(A * torch.eye(len(a), dtype=a.dtype, device=device) + B * a + C * (a @ a), parts)
         x = b @ x
         if i + 1 < iterations:
             x = rounded(x, parts)
-    return x.T if turned else x
+    return (x.t() if turned else x).cpu().numpy()
 
 
 def muon(p, g, m, lr, momentum, decay, iterations, nesterov, match_rms=False, parts=0):
