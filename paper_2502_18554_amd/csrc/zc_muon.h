@@ -239,7 +239,7 @@ __global__ __launch_bounds__(256) void muon_zeros_kernel(MuonArgs) {
 
 // ---- The products.  Workgroups of 2 x 2 waves make tiles of 64 T x 64 T results, a wave 32 T x 32 T.
 //
-// A stage is KB values of every row of the tile, brought straight to LDS; S stages lie there, of which one is multiplied while the others are on their way.  Rows follow each
+// A stage is 64 values (128 bytes) of every row of the tile, brought straight to LDS; S stages lie there, of which one is multiplied while the others are on their way.  Rows follow each
 // other in LDS, their 16-byte blocks exchanged by the row's number, so that 16 lanes that read LDS together find 64 different banks.  An instruction multiplies eight values of 32 rows with as
 // many of 32 columns from lanes 0 .. 31, eight others from lanes 32 .. 63.  Which column of the tile a lane brings is free: it is chosen so that a lane ends with 16
 // neighbouring results of a row.  The requests run ahead into the workgroup's next tile too.
@@ -267,10 +267,10 @@ struct MuonRows {
 __device__ inline void muon_load_to_lds(__amdgpu_buffer_rsrc_t from, u32 to, u32 lane_offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(lane_offset), "s"(from) : "memory");
 }
-// Keeps an instruction's sums at their place, in the matrix instructions' own registers where a wave has more of them than the others would hold.
-template <int OF>
+// Keeps an instruction's sums at their place, in the matrix instructions' own registers where a wave is alone on its SIMD (the compiler has them there then).
+template <bool OWN>
 __device__ __forceinline__ void muon_hold(f32x16_t& sum) {
-  if constexpr (OF > 4) asm volatile("" : "+a"(sum));
+  if constexpr (OWN) asm volatile("" : "+a"(sum));
   else asm volatile("" : "+v"(sum));
 }
 
@@ -342,8 +342,14 @@ struct MuonTurn {
   }
 };
 
+// Workgroups that a CU holds of a kernel with tiles of 64 T and S stages in LDS: a workgroup has a wave on each SIMD.
+constexpr int muon_groups(int T, int S) {
+  const int by_lds = 10 / (T * S);                   // (160 KiB, of which a stage takes 16 KiB T)
+  return T >= 3 || by_lds < 2 ? 1 : by_lds < 4 ? 2 : 4;
+}
+
 // The results of a wave, 32 T x 32 T from (row0, col0) on.  mirrored: those of a symmetric matrix off its diagonal, which go to the other half as well.
-template <int T, int MODE>
+template <int T, int MODE, bool ALONE>
 __device__ __forceinline__ void muon_results(const MuonArgs& a, const MuonOf& of, const MuonParts& parts, u64 row0, u64 col0, bool mirrored, f32x16_t (&sum)[T][T]) {
   u8* const at = of.at;
   const u32 r = of.r, c = of.c, lane = threadIdx.x & 63u, half = lane >> 5, in32 = lane & 31u;
@@ -363,7 +369,7 @@ __device__ __forceinline__ void muon_results(const MuonArgs& a, const MuonOf& of
     constexpr int i = decltype(number)::value;
     constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
-    for (int j = 0; j < T; ++j) muon_hold<T * T>(sum[i][j]);
+    for (int j = 0; j < T; ++j) muon_hold<ALONE>(sum[i][j]);
     const bool row_there = WHOLE || 32 * i + i32(in32) < rows_left;
     if constexpr (MODE >= kMuonFinish) {
       using One = typename ValueOf<MODE - kMuonFinish>::One;
@@ -507,16 +513,11 @@ __device__ __forceinline__ void muon_wait() {
   asm volatile("" ::: "memory");
 }
 
-// Waves that a SIMD holds of a kernel with tiles of 64 T and S stages of KB values in LDS: a workgroup has one on each.
-constexpr u32 muon_lds_bytes(int T, int KB, int S) { return u32(S) * 2 * 64 * T * KB * 2; }
-constexpr int muon_groups(int T, int KB, int S) { return T >= 3 ? 1 : int(163840u / muon_lds_bytes(T, KB, S)) < (T == 2 ? 2 : 4) ? int(163840u / muon_lds_bytes(T, KB, S)) : T == 2 ? 2 : 4; }
-
-template <int T, int KB, int S, int MODE>
-__global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : muon_groups(T, KB, S)) void muon_product_kernel(MuonArgs) {
+template <int T, int S, int MODE>
+__global__ __launch_bounds__(256, muon_groups(T, S)) void muon_product_kernel(MuonArgs) {
   const MuonArgs& a = kernel_args<MuonArgs, 0>();
-  constexpr u32 R = 64u * T, BLOCKS = KB / 8, ROW = 2 * KB, PLANE = R * ROW, STAGE = 2 * PLANE;      // bytes of a row, of an operand's rows, of a stage
+  constexpr u32 KB = 64, R = 64u * T, BLOCKS = KB / 8, ROW = 2 * KB, PLANE = R * ROW, STAGE = 2 * PLANE;      // bytes of a row, of an operand's rows, of a stage
   constexpr u32 APART = 4096 / ROW, LOADS = STAGE / 4096, STEPS = KB / 16;                           // rows between a thread's loads
-  static_assert(KB == 64 || KB == 128);
   __shared__ u32x4_t memory[S * STAGE / 16];
   const u32 tid = threadIdx.x, lane = tid & 63u, wave = uniform(tid >> 6), half = lane >> 5, in32 = lane & 31u;
   const MuonTiles<MODE> tiles(a.count);
@@ -527,8 +528,8 @@ __global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : m
   MuonRows rows_a, rows_b;
   const u32 my_row = tid / BLOCKS;
   // Which block of a row is where: the place's number exchanged by what tells the rows apart that are read together.
-  const auto key_a = [](u32 row) { return KB == 128 ? row & 15u : row >> 1 & 7u; };
-  const auto key_b = [](u32 row) { return KB == 128 ? (row & 7u) | (row >> 1 & 8u) : (row >> 1 & 1u) | (row >> 3 & 2u) | (row & 4u); };
+  const auto key_a = [](u32 row) { return row >> 1 & 7u; };
+  const auto key_b = [](u32 row) { return (row >> 1 & 1u) | (row >> 3 & 2u) | (row & 4u); };
   u32 mine_a[LOADS / 2], mine_b[LOADS / 2];          // a thread's places in the tile's rows
   const auto aim = [&] {
     const MuonOf of(a, ask_tile);
@@ -579,7 +580,6 @@ __global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : m
   const u32 lane_b = (in32 & 3u) + 16u * ((in32 >> 2) & 1u) + 4u * (in32 >> 3);
   // The blocks of this step and of the next two (one, where registers are short); in tiles of 64, where a step is one instruction, less than LDS takes to answer, those of this stage and of the next one.
   constexpr u32 AHEAD = T == 1 ? STEPS : T == 4 || (T == 3 && MODE == kMuonPoly) ? 1 : 2, HELD = T == 1 ? 2 * STEPS : STEPS;
-  static_assert(STEPS == 4 || T == 1);
   u32x4_t fa[HELD][T], fb[HELD][T];
   u32 at_a[STEPS], at_b[STEPS];                      // where a lane's block of step t is, in the first stage's place
 #pragma unroll
@@ -631,12 +631,7 @@ __global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : m
     if constexpr (T == 1) {
       for (u32 pair = 0; pair < stages; pair += 2) {
 #pragma unroll
-        for (u32 u = 0; u < 2; ++u) {
-          if (u && pair + 1 == stages) {               // an odd number of stages: what has been read for the next tile goes where that looks for it
-#pragma unroll
-            for (u32 t = 0; t < STEPS; ++t) fa[t][0] = fa[STEPS + t][0], fb[t][0] = fb[STEPS + t][0];
-            break;
-          }
+        for (u32 u = 0; u < 2; ++u) {                  // (of an even number of stages)
           const u32 next = behind(now);
 #pragma unroll
           for (u32 i = 0; i < EARLY; ++i) ask(free, EARLY + i);
@@ -675,7 +670,7 @@ __global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : m
               if (i * SLOTS / (2 * READS) == slot) read((t + AHEAD) % STEPS, t + AHEAD < STEPS ? now : next, (t + AHEAD) % STEPS, i);
             const u32 i = slot / T, j = slot % T;
             sum[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, fb[t][j]), __builtin_bit_cast(f16x8_t, fa[t][i]), sum[i][j], 0, 0, 0);
-            muon_hold<T * T>(sum[i][j]);
+            muon_hold<muon_groups(T, S) == 1>(sum[i][j]);
             __builtin_amdgcn_sched_barrier(0);
           }
           if (AHEAD == 1 && t == 0) next_stage();
@@ -689,7 +684,7 @@ __global__ __launch_bounds__(256, T >= 3 ? 1 : muon_groups(T, KB, S) < 2 ? 2 : m
     u32 down, across;
     const u32 tiles_down = (r + R - 1) / R, tiles_across = MODE == kMuonGram || MODE == kMuonPoly ? tiles_down : (c + R - 1) / R;
     MuonTiles<MODE>::place(tile - of.first, tiles_down, tiles_across, down, across);
-    muon_results<T, MODE>(a, of, parts, u64(down) * R + wave_a, u64(across) * R + wave_b, down != across, sum);
+    muon_results<T, MODE, muon_groups(T, S) == 1>(a, of, parts, u64(down) * R + wave_a, u64(across) * R + wave_b, down != across, sum);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (the last requests, too, before the workgroup's LDS is given to another one)
 }
@@ -778,7 +773,7 @@ __global__ __launch_bounds__(256, S == 2 ? 2 : 1) void muon_small_kernel(MuonArg
   if (wave) return;
 #pragma unroll
   for (int k = 0; k < 16; ++k) sum[0][0][k] = ((sum[0][0][k] + other[k]) + sums[(16 + k) * 64 + lane]) + (sums[(32 + k) * 64 + lane] + sums[(48 + k) * 64 + lane]);
-  muon_results<1, MODE>(a, of, parts, u64(down) * 32, u64(across) * 32, down != across, sum);
+  muon_results<1, MODE, false>(a, of, parts, u64(down) * 32, u64(across) * 32, down != across, sum);
 }
 
 }  // namespace zc

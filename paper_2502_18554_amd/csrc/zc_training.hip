@@ -138,16 +138,15 @@ void count_muon_tiles(MuonArgs& a, u64 side) {
   }
   if (a.each) a.each = a.count / a.tensors;
 }
-constexpr int muon_stages(int T) { return T == 3 ? 3 : T == 1 ? 4 : 2; }        // that lie in LDS
-template <int T, int MODE>
+template <int T, int S, int MODE>
 void launch_muon_tiles(MuonArgs& a, hipStream_t stream) {
   count_muon_tiles<MODE>(a, 64 * T);
-  const u32 at_once = 256 * muon_groups(T, 64, muon_stages(T));
-  hipLaunchKernelGGL((muon_product_kernel<T, 64, muon_stages(T), MODE>), dim3(a.count < at_once ? a.count : at_once), dim3(256), 0, stream, a);
+  const u32 at_once = 256 * muon_groups(T, S);
+  hipLaunchKernelGGL((muon_product_kernel<T, S, MODE>), dim3(a.count < at_once ? a.count : at_once), dim3(256), 0, stream, a);
 }
 // The size of tile that takes the least time, in us, by what a turn of all CUs has been measured to take: a tile's begin and end, and its stages of 64 values.
 // (X X^T of three matrices of 333 x 1531 in two parts: tiles of 32, 64 and 128 9.5, 21 and 33 us; 24 of 256 x 512: 8.4, 6.9 and 9.1; six of 1024 x 4096 in two parts, tiles of 64, 128, 192 and 256:
-// 146, 120, 141 and 223; 4096 x 8192, tiles of 128, 192 and 256: 181, 123 and 154.)
+// 146, 95, 141 and 223; 4096 x 8192, tiles of 128, 192 and 256: 181, 123 and 154.)
 template <int MODE>
 void launch_muon_product(MuonArgs& a, hipStream_t stream) {
   constexpr int SIDES = 5;
@@ -165,7 +164,7 @@ void launch_muon_product(MuonArgs& a, hipStream_t stream) {
   const auto turns = [&](int t, double at_once) { return std::ceil(tiles[t] / at_once); };
   const double cost[SIDES] = {2 + turns(0, 512) * (2.3 + (tiles[0] <= 512 ? 0.075 : 0.16) * stages(0)),
                               3 + (tiles[1] <= 256 ? 2 + 0.25 * stages(1) : turns(1, 512) * (3 + 0.5 * stages(1))),
-                              tiles[2] <= 256 ? 7 + 0.6 * stages(2) : 4 + turns(2, 512) * (12 + 1.1 * stages(2)),
+                              tiles[2] <= 256 ? 7 + 0.46 * stages(2) : 4 + turns(2, 512) * (12 + 1.1 * stages(2)),
                               turns(3, 256) * (12 + (tiles[3] <= 160 ? 0.68 : 0.83) * stages(3)),
                               turns(4, 256) * (22 + (tiles[4] <= 160 ? 1.1 : 1.4) * stages(4))};
   int best = 0;
@@ -175,13 +174,16 @@ void launch_muon_product(MuonArgs& a, hipStream_t stream) {
     count_muon_tiles<MODE>(a, 32);
     hipLaunchKernelGGL((muon_small_kernel<2, MODE>), dim3(a.count), dim3(256), 0, stream, a);
   } else if (best == 1) {
-    launch_muon_tiles<1, MODE>(a, stream);
+    launch_muon_tiles<1, 4, MODE>(a, stream);
   } else if (best == 2) {
-    launch_muon_tiles<2, MODE>(a, stream);
+    // Where every CU has one tile at most, a third stage lies in LDS instead of a second workgroup's (X X^T of six matrices of 1024 x 4096 in two parts, 216 tiles, 95 us, 126 by two;
+    // of 4096 x 8192, 528 tiles, 181 by two).
+    if (tiles[2] <= 256) launch_muon_tiles<2, 3, MODE>(a, stream);
+    else launch_muon_tiles<2, 2, MODE>(a, stream);
   } else if (best == 3) {
-    launch_muon_tiles<3, MODE>(a, stream);
+    launch_muon_tiles<3, 3, MODE>(a, stream);
   } else if constexpr (MODE != kMuonPoly) {
-    launch_muon_tiles<4, MODE>(a, stream);
+    launch_muon_tiles<4, 2, MODE>(a, stream);
   }
 }
 
