@@ -68,6 +68,9 @@ __global__ __launch_bounds__(norm_threads<T>()) void norm_kernel(NormArgs a) {
   const u32 t = threadIdx.x % T, group = threadIdx.x / T;
   const u32 mine = values_of_lanes<T, P>(a.cols, T < 64 ? 0u : t & ~63u);
   const float per_mine = mine ? 1.0f / float(mine) : 0.0f, per_row = 1.0f / float(a.cols);
+  // A lane brings one of the waves' sums together with the others': how many values that wave has.
+  const u32 of_wave = t & 15u;
+  const float its = T > 64 && of_wave < T / 64 ? float(values_of_lanes<T, P>(a.cols, 64 * of_wave)) : 0.0f, per_its = its > 0.0f ? 1.0f / its : 0.0f;
   i32 left[P];
   float w[P][8], b[P][8];
 #pragma unroll
@@ -114,18 +117,10 @@ __global__ __launch_bounds__(norm_threads<T>()) void norm_kernel(NormArgs a) {
     if constexpr (T > 64) {
       if ((t & 63u) == 0) exchange.slot[parity][t >> 6] = make_float2(sum, squares);
       __syncthreads();
-      sum = 0.0f;
-#pragma unroll
-      for (int k = 0; k < T / 64; ++k) sum += exchange.slot[parity][k].x;
-      mean = sum * per_row;
-      squares = 0.0f;
-#pragma unroll
-      for (u32 k = 0; k < T / 64; ++k) {
-        const float2 of = exchange.slot[parity][k];
-        const u32 n = values_of_lanes<T, P>(a.cols, 64 * k);
-        const float off = n ? of.x / float(n) - mean : 0.0f;
-        squares += __builtin_fmaf(off * off, float(n), of.y);
-      }
+      const float2 of = of_wave < T / 64 ? exchange.slot[parity][of_wave] : make_float2(0.0f, 0.0f);
+      mean = sum_of_16(of.x) * per_row;
+      const float off = of.x * per_its - mean;
+      squares = sum_of_16(__builtin_fmaf(off * off, its, of.y));
       parity ^= 1u;
     }
     const float d = 1.0f / sqrtf(__builtin_fmaf(squares, per_row, a.eps));
@@ -217,12 +212,10 @@ __global__ __launch_bounds__(norm_threads<T>()) void norm_backward_kernel(NormBa
     if constexpr (T > 64) {
       if ((t & 63u) == 0) lds.exchange.slot[parity][t >> 6] = make_float2(one, two);
       __syncthreads();
-      one = two = 0.0f;
-#pragma unroll
-      for (int k = 0; k < T / 64; ++k) {
-        one += lds.exchange.slot[parity][k].x;
-        two += lds.exchange.slot[parity][k].y;
-      }
+      const u32 of_wave = t & 15u;
+      const float2 of = of_wave < T / 64 ? lds.exchange.slot[parity][of_wave] : make_float2(0.0f, 0.0f);
+      one = sum_of_16(of.x);
+      two = sum_of_16(of.y);
       parity ^= 1u;
     }
     one *= per_row;

@@ -12,7 +12,13 @@ template <> struct RawEight<false> { u32 w[4]; };
 struct __attribute__((packed, aligned(4))) F32EightAt { u32 w[8]; };
 struct __attribute__((packed, aligned(2))) B16EightAt { u32 w[4]; };
 
-// The first `left` of them (8 and more: all, 0 and less: none); zeros behind.
+struct __attribute__((packed, aligned(4))) W4At { u32 w[4]; };
+struct __attribute__((packed, aligned(4))) W2At { u32 w[2]; };
+struct __attribute__((packed, aligned(2))) H4At { u32 w[2]; };
+struct __attribute__((packed, aligned(2))) H2At { u32 w; };
+
+// The first `left` of them (8 and more: all, 0 and less: none); zeros behind.  The end of a row comes by four, two and one: few instructions, for kernels that run for a few us wait for
+// instructions that they have not seen yet.
 template <bool WIDE>
 __device__ inline RawEight<WIDE> load_eight(const void* base, u64 at, i32 left) {
   RawEight<WIDE> r = {};
@@ -27,11 +33,27 @@ __device__ inline RawEight<WIDE> load_eight(const void* base, u64 at, i32 left) 
       for (int j = 0; j < 4; ++j) r.w[j] = v.w[j];
     }
   } else if (left > 0) {
+    const bool four = left & 4, two = left & 2, one = left & 1;
+    if constexpr (WIDE) {
+      const u32* const from = static_cast<const u32*>(base) + at;
+      const W4At a = four ? *reinterpret_cast<const W4At*>(from) : W4At{};
+      const W2At b = two ? *reinterpret_cast<const W2At*>(from + (left & 4)) : W2At{};
+      const u32 c = one ? from[left & 6] : 0u;
+      const u32 next[3] = {two ? b.w[0] : c, b.w[1], two ? c : 0u};
 #pragma unroll
-    for (int j = 0; j < 7; ++j) {
-      if (j >= left) continue;
-      if constexpr (WIDE) r.w[j] = static_cast<const u32*>(base)[at + j];
-      else r.w[j / 2] |= u32(static_cast<const u16*>(base)[at + j]) << (16 * (j & 1));
+      for (int j = 0; j < 4; ++j) r.w[j] = four ? a.w[j] : j < 3 ? next[j] : 0u;
+#pragma unroll
+      for (int j = 0; j < 3; ++j) r.w[4 + j] = four ? next[j] : 0u;
+    } else {
+      const u16* const from = static_cast<const u16*>(base) + at;
+      const H4At a = four ? *reinterpret_cast<const H4At*>(from) : H4At{};
+      const u32 b = two ? reinterpret_cast<const H2At*>(from + (left & 4))->w : 0u, c = one ? u32(from[left & 6]) : 0u;
+      const u32 next[2] = {two ? b : c, two ? c : 0u};
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        r.w[j] = four ? a.w[j] : next[j];
+        r.w[2 + j] = four ? next[j] : 0u;
+      }
     }
   }
   return r;
@@ -91,11 +113,19 @@ __device__ inline void store_raw_eight(void* base, u64 at, i32 left, const RawEi
       *reinterpret_cast<B16EightAt*>(static_cast<u16*>(base) + at) = v;
     }
   } else if (left > 0) {
-#pragma unroll
-    for (int j = 0; j < 7; ++j) {
-      if (j >= left) continue;
-      if constexpr (WIDE) static_cast<u32*>(base)[at + j] = r.w[j];
-      else static_cast<u16*>(base)[at + j] = u16(r.w[j / 2] >> (16 * (j & 1)));
+    const bool four = left & 4, two = left & 2;
+    if constexpr (WIDE) {
+      u32* const to = static_cast<u32*>(base) + at;
+      if (four) *reinterpret_cast<W4At*>(to) = W4At{{r.w[0], r.w[1], r.w[2], r.w[3]}};
+      const u32 next[3] = {four ? r.w[4] : r.w[0], four ? r.w[5] : r.w[1], four ? r.w[6] : r.w[2]};
+      if (two) *reinterpret_cast<W2At*>(to + (left & 4)) = W2At{{next[0], next[1]}};
+      if (left & 1) to[left & 6] = two ? next[2] : next[0];
+    } else {
+      u16* const to = static_cast<u16*>(base) + at;
+      if (four) *reinterpret_cast<H4At*>(to) = H4At{{r.w[0], r.w[1]}};
+      const u32 next[2] = {four ? r.w[2] : r.w[0], four ? r.w[3] : r.w[1]};
+      if (two) reinterpret_cast<H2At*>(to + (left & 4))->w = next[0];
+      if (left & 1) to[left & 6] = u16(two ? next[1] : next[0]);
     }
   }
 }
