@@ -237,7 +237,7 @@ __global__ __launch_bounds__(256) void muon_zeros_kernel(MuonArgs) {
   clear(parts.b, parts.plane_a);
 }
 
-// ---- The products.  Workgroups of 2 x 2 waves make tiles of 64 T x 64 T results, a wave 32 T x 32 T.
+// ---- The products.  Workgroups of 2 x 2 waves make tiles of 64 TM x 64 TN results, a wave 32 TM x 32 TN.
 //
 // A stage is 64 values (128 bytes) of every row of the tile, brought straight to LDS; S stages lie there, of which one is multiplied while the others are on their way.  Rows follow each
 // other in LDS, their 16-byte blocks exchanged by the row's number, so that 16 lanes that read LDS together find 64 different banks.  An instruction multiplies eight values of 32 rows with as
@@ -342,15 +342,15 @@ struct MuonTurn {
   }
 };
 
-// Workgroups that a CU holds of a kernel with tiles of 64 T and S stages in LDS: a workgroup has a wave on each SIMD.
-constexpr int muon_groups(int T, int S) {
-  const int by_lds = 10 / (T * S);                   // (160 KiB, of which a stage takes 16 KiB T)
-  return T >= 3 || by_lds < 2 ? 1 : by_lds < 4 ? 2 : 4;
+// Workgroups that a CU holds of a kernel with tiles of 64 TM x 64 TN and S stages in LDS: a workgroup has a wave on each SIMD.
+constexpr int muon_groups(int TM, int TN, int S) {
+  const int by_lds = 20 / ((TM + TN) * S);           // (160 KiB, of which a stage takes 8 KiB (TM + TN))
+  return TM * TN > 4 || by_lds < 2 ? 1 : by_lds < 4 ? 2 : 4;
 }
 
-// The results of a wave, 32 T x 32 T from (row0, col0) on.  mirrored: those of a symmetric matrix off its diagonal, which go to the other half as well.
-template <int T, int MODE, bool ALONE>
-__device__ __forceinline__ void muon_results(const MuonArgs& a, const MuonOf& of, const MuonParts& parts, u64 row0, u64 col0, bool mirrored, f32x16_t (&sum)[T][T]) {
+// The results of a wave, 32 TM x 32 TN from (row0, col0) on.  mirrored: those of a symmetric matrix off its diagonal, which go to the other half as well.
+template <int TM, int TN, int MODE, bool ALONE>
+__device__ __forceinline__ void muon_results(const MuonArgs& a, const MuonOf& of, const MuonParts& parts, u64 row0, u64 col0, bool mirrored, f32x16_t (&sum)[TM][TN]) {
   u8* const at = of.at;
   const u32 r = of.r, c = of.c, lane = threadIdx.x & 63u, half = lane >> 5, in32 = lane & 31u;
   const u32 planes = a.planes, which = a.which;
@@ -369,16 +369,16 @@ __device__ __forceinline__ void muon_results(const MuonArgs& a, const MuonOf& of
     constexpr int i = decltype(number)::value;
     constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
-    for (int j = 0; j < T; ++j) muon_hold<ALONE>(sum[i][j]);
+    for (int j = 0; j < TN; ++j) muon_hold<ALONE>(sum[i][j]);
     const bool row_there = WHOLE || 32 * i + i32(in32) < rows_left;
     if constexpr (MODE >= kMuonFinish) {
       using One = typename ValueOf<MODE - kMuonFinish>::One;
       constexpr bool WIDE = MODE == kMuonFinish + ZC_F32;
       One* const param = static_cast<One*>(params);
       // (Two blocks at a time: registers are short.)
-      constexpr int TOGETHER = T < 2 ? T : 2;
+      constexpr int TOGETHER = TN < 2 ? TN : 2;
 #pragma unroll
-      for (int j0 = 0; j0 < T; j0 += TOGETHER) {
+      for (int j0 = 0; j0 < TN; j0 += TOGETHER) {
         if (turned) {
           const u64 first = (col0 + 16 * half) * r + row0 + 32 * i + in32;
           One old[TOGETHER][16];
@@ -387,15 +387,15 @@ __device__ __forceinline__ void muon_results(const MuonArgs& a, const MuonOf& of
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
               const int at_col = 32 * (j0 + d) + k;
-              old[d][k] = j0 + d < T && row_there && (WHOLE || at_col + 16 * i32(half) < cols_left) ? param[first + u64(at_col) * r] : One(0.0f);
+              old[d][k] = j0 + d < TN && row_there && (WHOLE || at_col + 16 * i32(half) < cols_left) ? param[first + u64(at_col) * r] : One(0.0f);
             }
 #pragma unroll
           for (int d = 0; d < TOGETHER; ++d)
-            if (j0 + d < T) {
+            if (j0 + d < TN) {
 #pragma unroll
               for (int k = 0; k < 16; ++k) {
                 const int at_col = 32 * (j0 + d) + k;
-                const float p = __builtin_fmaf(step, sum[i][j0 + d < T ? j0 + d : 0][k], float(old[d][k]) * keep);
+                const float p = __builtin_fmaf(step, sum[i][j0 + d < TN ? j0 + d : 0][k], float(old[d][k]) * keep);
                 if (row_there && (WHOLE || at_col + 16 * i32(half) < cols_left)) {
                   param[first + u64(at_col) * r] = One(p);
                   if (copy) store_value(copy, copy_type, first + u64(at_col) * r, p);
@@ -405,21 +405,21 @@ __device__ __forceinline__ void muon_results(const MuonArgs& a, const MuonOf& of
         } else {
           const u64 first = (row0 + 32 * i + in32) * c + col0 + 16 * half;
           RawEight<WIDE> old[TOGETHER][2];
-          const auto left_of_piece = [&](int j, int h) { return WHOLE ? 8 : row_there && j < T ? cols_left - 32 * j - 16 * i32(half) - 8 * h : 0; };
+          const auto left_of_piece = [&](int j, int h) { return WHOLE ? 8 : row_there && j < TN ? cols_left - 32 * j - 16 * i32(half) - 8 * h : 0; };
 #pragma unroll
           for (int d = 0; d < TOGETHER; ++d)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              if (j0 + d < T) old[d][h] = load_eight<WIDE>(param, first + 32 * (j0 + d) + 8 * h, left_of_piece(j0 + d, h));
+              if (j0 + d < TN) old[d][h] = load_eight<WIDE>(param, first + 32 * (j0 + d) + 8 * h, left_of_piece(j0 + d, h));
 #pragma unroll
           for (int d = 0; d < TOGETHER; ++d)
-            if (j0 + d < T) {
+            if (j0 + d < TN) {
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
                 float p[8];
                 numbers_of<WIDE>(old[d][h], MODE - kMuonFinish, p);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) p[k] = __builtin_fmaf(step, sum[i][j0 + d < T ? j0 + d : 0][8 * h + k], p[k] * keep);
+                for (int k = 0; k < 8; ++k) p[k] = __builtin_fmaf(step, sum[i][j0 + d < TN ? j0 + d : 0][8 * h + k], p[k] * keep);
                 store_eight<WIDE>(param, MODE - kMuonFinish, first + 32 * (j0 + d) + 8 * h, left_of_piece(j0 + d, h), p);
                 if (copy) store_numbers(copy, copy_type, first + 32 * (j0 + d) + 8 * h, left_of_piece(j0 + d, h), p);
               }
@@ -435,14 +435,14 @@ __device__ __forceinline__ void muon_results(const MuonArgs& a, const MuonOf& of
       const auto there = [&](int j, int q) { return WHOLE || (32 * i + 16 * q + i32(lane & 15u) < rows_left && 32 * j + 8 * i32(lane >> 4) < along_left); };
       const auto there_turned = [&](int j, int m) { return WHOLE || (32 * i + i32(in32 & ~3u) < rows_left && 32 * j + 16 * i32(half) + 4 * m + i32(lane & 3u) < cols_left); };
       const u64 plane_to = OF_X ? parts.plane_x : parts.plane_a, plane_turned = OF_X ? parts.plane_t : parts.plane_a;
-      u32 old[MODE == kMuonPoly ? T : 1][2][8];
+      u32 old[MODE == kMuonPoly ? TN : 1][2][8];
       if constexpr (MODE == kMuonPoly) {
         const u8* const from = at + uniform64(parts.a + 2 * ((row0 + 32 * i) * along + col0));
 #pragma unroll
         for (u32 plane = 0; plane < 2; ++plane)
           if (plane < planes) {
 #pragma unroll
-            for (int j = 0; j < T; ++j)
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
               for (int q = 0; q < 2; ++q) {
                 const u32x4_t p = there(j, q) ? *reinterpret_cast<const u32x4_t*>(at_bytes(from + plane * parts.plane_a + 32 * q * along + 64 * j, mine)) : u32x4_t{};
@@ -452,7 +452,7 @@ __device__ __forceinline__ void muon_results(const MuonArgs& a, const MuonOf& of
           }
       }
 #pragma unroll
-      for (int j = 0; j < T; ++j) {
+      for (int j = 0; j < TN; ++j) {
         float v[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) v[k] = sum[i][j][k] * (MODE == kMuonPoly ? kMuonC / kMuonScale : 1.0f / kMuonScale);
@@ -499,9 +499,9 @@ __device__ __forceinline__ void muon_results(const MuonArgs& a, const MuonOf& of
     }
   };
   const auto all_rows = [&](auto whole) __attribute__((always_inline)) {
-    [&]<int... N>(std::integer_sequence<int, N...>) { (row_of_blocks(std::integral_constant<int, N>(), whole), ...); }(std::make_integer_sequence<int, T>());
+    [&]<int... N>(std::integer_sequence<int, N...>) { (row_of_blocks(std::integral_constant<int, N>(), whole), ...); }(std::make_integer_sequence<int, TM>());
   };
-  if (rows_left >= 32 * T && cols_left >= 32 * T) all_rows(std::true_type());
+  if (rows_left >= 32 * TM && cols_left >= 32 * TN) all_rows(std::true_type());
   else all_rows(std::false_type());
 }
 
@@ -513,11 +513,13 @@ __device__ __forceinline__ void muon_wait() {
   asm volatile("" ::: "memory");
 }
 
-template <int T, int S, int MODE>
-__global__ __launch_bounds__(256, muon_groups(T, S)) void muon_product_kernel(MuonArgs) {
+template <int TM, int TN, int S, int MODE>
+__global__ __launch_bounds__(256, muon_groups(TM, TN, S)) void muon_product_kernel(MuonArgs) {
   const MuonArgs& a = kernel_args<MuonArgs, 0>();
-  constexpr u32 KB = 64, R = 64u * T, BLOCKS = KB / 8, ROW = 2 * KB, PLANE = R * ROW, STAGE = 2 * PLANE;      // bytes of a row, of an operand's rows, of a stage
-  constexpr u32 APART = 4096 / ROW, LOADS = STAGE / 4096, STEPS = KB / 16;                           // rows between a thread's loads
+  constexpr u32 KB = 64, RA = 64u * TM, RB = 64u * TN, BLOCKS = KB / 8, ROW = 2 * KB, AT_B = RA * ROW, STAGE = AT_B + RB * ROW;      // bytes of a row, of a stage
+  constexpr u32 APART = 4096 / ROW, LOADS_A = AT_B / 4096, LOADS = STAGE / 4096, STEPS = KB / 16;    // rows between a thread's loads; its loads
+  constexpr bool TRIANGLE = MODE == kMuonGram || MODE == kMuonPoly, SMALL = TM * TN == 1;
+  static_assert(!TRIANGLE || TM == TN);
   __shared__ u32x4_t memory[S * STAGE / 16];
   const u32 tid = threadIdx.x, lane = tid & 63u, wave = uniform(tid >> 6), half = lane >> 5, in32 = lane & 31u;
   const MuonTiles<MODE> tiles(a.count);
@@ -530,27 +532,27 @@ __global__ __launch_bounds__(256, muon_groups(T, S)) void muon_product_kernel(Mu
   // Which block of a row is where: the place's number exchanged by what tells the rows apart that are read together.
   const auto key_a = [](u32 row) { return row >> 1 & 7u; };
   const auto key_b = [](u32 row) { return (row >> 1 & 1u) | (row >> 3 & 2u) | (row & 4u); };
-  u32 mine_a[LOADS / 2], mine_b[LOADS / 2];          // a thread's places in the tile's rows
+  u32 mine_a[LOADS_A], mine_b[LOADS - LOADS_A];          // a thread's places in the tile's rows
   const auto aim = [&] {
     const MuonOf of(a, ask_tile);
     const u32 r = of.r, c = of.c;
     const MuonParts parts(r, c, a.planes);
     u32 row, col;
-    const u32 down = (r + R - 1) / R, across = MODE == kMuonGram || MODE == kMuonPoly ? down : (c + R - 1) / R;
+    const u32 down = (r + RA - 1) / RA, across = TRIANGLE ? down : (c + RB - 1) / RB;
     MuonTiles<MODE>::place(ask_tile - of.first, down, across, row, col);
     const u8* const at = of.at;
     const u64 plane_a = MODE == kMuonGram ? parts.plane_x : parts.plane_a, plane_b = MODE == kMuonGram ? parts.plane_x : MODE == kMuonPoly ? parts.plane_a : parts.plane_t;
     const u8* const from_a = at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : parts.b) + (ask_segment == 2 ? plane_a : 0);
     const u8* const from_b = at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : a.which ? parts.t1 : parts.t0) + (ask_segment == 1 ? plane_b : 0);
     const u64 along = MODE == kMuonGram ? parts.row_x : parts.row_t;
-    rows_a.aim(from_a, u64(row) * R, r, 2 * along, R);
-    rows_b.aim(from_b, u64(col) * R, MODE == kMuonGram || MODE == kMuonPoly ? r : c, 2 * along, R);
+    rows_a.aim(from_a, u64(row) * RA, r, 2 * along, RA);
+    rows_b.aim(from_b, u64(col) * RB, TRIANGLE ? r : c, 2 * along, RB);
     const u32 apart = uniform(u32(2 * along));
 #pragma unroll
-    for (u32 k = 0; k < LOADS / 2; ++k) {
-      const u32 of = my_row + APART * k;
-      mine_a[k] = of * apart + 16u * ((tid ^ key_a(of)) & (BLOCKS - 1));
-      mine_b[k] = of * apart + 16u * ((tid ^ key_b(of)) & (BLOCKS - 1));
+    for (u32 k = 0; k < LOADS; ++k) {
+      const u32 of = my_row + APART * (k < LOADS_A ? k : k - LOADS_A);
+      if (k < LOADS_A) mine_a[k] = of * apart + 16u * ((tid ^ key_a(of)) & (BLOCKS - 1));
+      else mine_b[k - LOADS_A] = of * apart + 16u * ((tid ^ key_b(of)) & (BLOCKS - 1));
     }
     ask_stages = uniform(u32(along / KB));
   };
@@ -572,34 +574,34 @@ __global__ __launch_bounds__(256, muon_groups(T, S)) void muon_product_kernel(Mu
   const u32 lds0 = u32(reinterpret_cast<uintptr_t>((LdsWord*)&memory[0]));
   const auto ask = [&](u32 place, u32 i) {           // place: of the stage in LDS, in bytes
     const u32 to = lds0 + wave * 1024u + place + 4096u * i;
-    if (i < LOADS / 2) muon_load_to_lds(rows_a.buffer(), to, mine_a[i]);
-    else muon_load_to_lds(rows_b.buffer(), to, mine_b[i - LOADS / 2]);
+    if (i < LOADS_A) muon_load_to_lds(rows_a.buffer(), to, mine_a[i]);
+    else muon_load_to_lds(rows_b.buffer(), to, mine_b[i - LOADS_A]);
   };
 
-  const u32 wave_a = (wave >> 1) * 32u * T, wave_b = (wave & 1u) * 32u * T;
+  const u32 wave_a = (wave >> 1) * 32u * TM, wave_b = (wave & 1u) * 32u * TN;
   const u32 lane_b = (in32 & 3u) + 16u * ((in32 >> 2) & 1u) + 4u * (in32 >> 3);
   // The blocks of this step and of the next two (one, where registers are short); in tiles of 64, where a step is one instruction, less than LDS takes to answer, those of this stage and of the next one.
-  constexpr u32 AHEAD = T == 1 ? STEPS : T == 4 || (T == 3 && MODE == kMuonPoly) ? 1 : 2, HELD = T == 1 ? 2 * STEPS : STEPS;
-  u32x4_t fa[HELD][T], fb[HELD][T];
+  constexpr u32 AHEAD = SMALL ? STEPS : TM * TN > 9 || (TM * TN > 4 && MODE == kMuonPoly) ? 1 : 2, HELD = SMALL ? 2 * STEPS : STEPS;
+  u32x4_t fa[HELD][TM], fb[HELD][TN];
   u32 at_a[STEPS], at_b[STEPS];                      // where a lane's block of step t is, in the first stage's place
 #pragma unroll
   for (u32 t = 0; t < STEPS; ++t) {
     at_a[t] = lds0 + (wave_a + in32) * ROW + 16u * ((STEPS * half + t) ^ key_a(in32));
-    at_b[t] = lds0 + PLANE + (wave_b + lane_b) * ROW + 16u * ((STEPS * half + t) ^ key_b(lane_b));
+    at_b[t] = lds0 + AT_B + (wave_b + lane_b) * ROW + 16u * ((STEPS * half + t) ^ key_b(lane_b));
   }
   typedef const __attribute__((address_space(3))) u32x4_t LdsBlock;
   const auto read = [&](u32 to, u32 place, u32 t, u32 i) {
-    if (i < T) fa[to][i] = *reinterpret_cast<LdsBlock*>(at_a[t] + place + 32 * ROW * i);
-    else fb[to][i - T] = *reinterpret_cast<LdsBlock*>(at_b[t] + place + 32 * ROW * (i - T));
+    if (i < TM) fa[to][i] = *reinterpret_cast<LdsBlock*>(at_a[t] + place + 32 * ROW * i);
+    else fb[to][i - TM] = *reinterpret_cast<LdsBlock*>(at_b[t] + place + 32 * ROW * (i - TM));
   };
 
   // The instructions of a step and what goes between them: in the first half the reads for the steps to come; once everybody has read a stage, half of the requests for the one that takes
   // its place, and the other half in the step behind that.
-  constexpr u32 SLOTS = T * T, READS = 2 * T, EARLY = LOADS / 2;
+  constexpr u32 SLOTS = TM * TN, READS = TM + TN, EARLY = LOADS / 2;
   aim();
   const auto behind = [](u32 place) { return place + STAGE == S * STAGE ? 0u : place + STAGE; };
   u32 now = 0, free = 0;                             // the stage that is multiplied; the one that is asked for
-  constexpr int FIRST = T == 1 || AHEAD == 1 ? S - 1 : S;    // stages that are asked for before the first one is multiplied
+  constexpr int FIRST = SMALL || AHEAD == 1 ? S - 1 : S;    // stages that are asked for before the first one is multiplied
 #pragma unroll
   for (int s = 0; s < FIRST; ++s) {
 #pragma unroll
@@ -608,7 +610,7 @@ __global__ __launch_bounds__(256, muon_groups(T, S)) void muon_product_kernel(Mu
     free = behind(free);
   }
   muon_wait<(FIRST - 1) * int(LOADS)>();
-  if constexpr (T == 1 || AHEAD == 1) {
+  if constexpr (SMALL || AHEAD == 1) {
 #pragma unroll
     for (u32 i = 0; i < EARLY; ++i) ask(free, i);
   }
@@ -621,14 +623,14 @@ __global__ __launch_bounds__(256, muon_groups(T, S)) void muon_product_kernel(Mu
     const u32 r = of.r, c = of.c;
     const MuonParts parts(r, c, a.planes);
     const u32 stages = uniform(u32((MODE == kMuonGram ? parts.row_x : parts.row_t) / KB) * (a.planes > 1 ? 3u : 1u));
-    f32x16_t sum[T][T];
+    f32x16_t sum[TM][TN];
 #pragma unroll
-    for (int i = 0; i < T; ++i)
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int j = 0; j < T; ++j)
+      for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int k = 0; k < 16; ++k) sum[i][j][k] = 0.0f;
-    if constexpr (T == 1) {
+    if constexpr (SMALL) {
       for (u32 pair = 0; pair < stages; pair += 2) {
 #pragma unroll
         for (u32 u = 0; u < 2; ++u) {                  // (of an even number of stages)
@@ -668,9 +670,9 @@ __global__ __launch_bounds__(256, muon_groups(T, S)) void muon_product_kernel(Mu
 #pragma unroll
             for (u32 i = 0; i < READS; ++i)
               if (i * SLOTS / (2 * READS) == slot) read((t + AHEAD) % STEPS, t + AHEAD < STEPS ? now : next, (t + AHEAD) % STEPS, i);
-            const u32 i = slot / T, j = slot % T;
+            const u32 i = slot / TN, j = slot % TN;
             sum[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, fb[t][j]), __builtin_bit_cast(f16x8_t, fa[t][i]), sum[i][j], 0, 0, 0);
-            muon_hold<muon_groups(T, S) == 1>(sum[i][j]);
+            muon_hold<muon_groups(TM, TN, S) == 1>(sum[i][j]);
             __builtin_amdgcn_sched_barrier(0);
           }
           if (AHEAD == 1 && t == 0) next_stage();
@@ -682,9 +684,9 @@ __global__ __launch_bounds__(256, muon_groups(T, S)) void muon_product_kernel(Mu
     }
     // The results.
     u32 down, across;
-    const u32 tiles_down = (r + R - 1) / R, tiles_across = MODE == kMuonGram || MODE == kMuonPoly ? tiles_down : (c + R - 1) / R;
+    const u32 tiles_down = (r + RA - 1) / RA, tiles_across = TRIANGLE ? tiles_down : (c + RB - 1) / RB;
     MuonTiles<MODE>::place(tile - of.first, tiles_down, tiles_across, down, across);
-    muon_results<T, MODE, muon_groups(T, S) == 1>(a, of, parts, u64(down) * R + wave_a, u64(across) * R + wave_b, down != across, sum);
+    muon_results<TM, TN, MODE, muon_groups(TM, TN, S) == 1>(a, of, parts, u64(down) * RA + wave_a, u64(across) * RB + wave_b, down != across, sum);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (the last requests, too, before the workgroup's LDS is given to another one)
 }
@@ -773,7 +775,7 @@ __global__ __launch_bounds__(256, S == 2 ? 2 : 1) void muon_small_kernel(MuonArg
   if (wave) return;
 #pragma unroll
   for (int k = 0; k < 16; ++k) sum[0][0][k] = ((sum[0][0][k] + other[k]) + sums[(16 + k) * 64 + lane]) + (sums[(32 + k) * 64 + lane] + sums[(48 + k) * 64 + lane]);
-  muon_results<1, MODE, false>(a, of, parts, u64(down) * 32, u64(across) * 32, down != across, sum);
+  muon_results<1, 1, MODE, false>(a, of, parts, u64(down) * 32, u64(across) * 32, down != across, sum);
 }
 
 }  // namespace zc

@@ -124,66 +124,77 @@ u64 muon_workspace(int k, const size_t* rows, const size_t* cols, u32 planes) {
   return most;
 }
 
-u64 muon_tiles(const MuonTensor& t, int mode, u64 side) {
-  const u64 down = (t.r + side - 1) / side, across = (t.c + side - 1) / side;
+u64 muon_tiles(const MuonTensor& t, int mode, u64 high, u64 wide) {
+  const u64 down = (t.r + high - 1) / high, across = (t.c + wide - 1) / wide;
   return mode == kMuonGram || mode == kMuonPoly ? down * (down + 1) / 2 : down * across;
 }
-// Calls of tiles of `side`, in ascending order of the matrices.
 template <int MODE>
-void count_muon_tiles(MuonArgs& a, u64 side) {
+void count_muon_tiles(MuonArgs& a, u64 high, u64 wide) {
   a.count = 0;
   for (u32 i = 0; i < a.tensors; ++i) {
     a.first[i] = a.count;
-    a.count += u32(muon_tiles(a.t[i], MODE, side));
+    a.count += u32(muon_tiles(a.t[i], MODE, high, wide));
   }
   if (a.each) a.each = a.count / a.tensors;
 }
-template <int T, int S, int MODE>
+template <int TM, int TN, int S, int MODE>
 void launch_muon_tiles(MuonArgs& a, hipStream_t stream) {
-  count_muon_tiles<MODE>(a, 64 * T);
-  const u32 at_once = 256 * muon_groups(T, S);
-  hipLaunchKernelGGL((muon_product_kernel<T, S, MODE>), dim3(a.count < at_once ? a.count : at_once), dim3(256), 0, stream, a);
+  count_muon_tiles<MODE>(a, 64 * TM, 64 * TN);
+  const u32 at_once = 256 * muon_groups(TM, TN, S);
+  hipLaunchKernelGGL((muon_product_kernel<TM, TN, S, MODE>), dim3(a.count < at_once ? a.count : at_once), dim3(256), 0, stream, a);
 }
-// The size of tile that takes the least time, in us, by what a turn of all CUs has been measured to take: a tile's begin and end, and its stages of 64 values.
-// (X X^T of three matrices of 333 x 1531 in two parts: tiles of 32, 64 and 128 9.5, 21 and 33 us; 24 of 256 x 512: 8.4, 6.9 and 9.1; six of 1024 x 4096 in two parts, tiles of 64, 128, 192 and 256:
-// 146, 95, 141 and 223; 4096 x 8192, tiles of 128, 192 and 256: 181, 123 and 154.)
+// The kind of tile that takes the least time, in us, by what a turn of all CUs has been measured to take: a tile's begin and end, and its stages of 64 values.
+// (X X^T of three matrices of 333 x 1531 in two parts: tiles of 32, 64 and 128 9.5, 21 and 33 us, and the third product by 64, 64 x 128 and 128 17.7, 13.6 and 18.3; X X^T of 24 of 256 x 512 8.4,
+// 6.9 and 9.1.  Six of 1024 x 4096 in two parts, X X^T by tiles of 64, 128, 192 and 256 146, 95, 141 and 223, the third product by 128, 128 x 256, 192 and 256 209, 175, 208 and 184;
+// 4096 x 8192: X X^T by 128, 192 and 256 181, 123 and 154, the third product 252, 247 and 215.)
+struct MuonKind {
+  u64 high, wide;
+};
+constexpr MuonKind kMuonKinds[] = {{32, 32}, {64, 64}, {128, 128}, {192, 192}, {256, 256}, {64, 128}, {128, 256}};
+constexpr int kMuonKindsOf = 7;
 template <int MODE>
 void launch_muon_product(MuonArgs& a, hipStream_t stream) {
-  constexpr int SIDES = 5;
-  constexpr u64 sides[SIDES] = {32, 64, 128, 192, 256};
-  double tiles[SIDES] = {}, along[SIDES] = {};
+  double tiles[kMuonKindsOf] = {}, along[kMuonKindsOf] = {};
   for (u32 i = 0; i < a.tensors; ++i) {
     const double stages = double(muon_along(MODE == kMuonGram ? a.t[i].c : a.t[i].r)) / 64 * (a.planes > 1 ? 3 : 1);
-    for (int t = 0; t < SIDES; ++t) {
-      const double of_this = double(muon_tiles(a.t[i], MODE, sides[t]));
+    for (int t = 0; t < kMuonKindsOf; ++t) {
+      const double of_this = double(muon_tiles(a.t[i], MODE, kMuonKinds[t].high, kMuonKinds[t].wide));
       tiles[t] += of_this;
       along[t] += of_this * stages;
     }
   }
   const auto stages = [&](int t) { return along[t] / tiles[t]; };
   const auto turns = [&](int t, double at_once) { return std::ceil(tiles[t] / at_once); };
-  const double cost[SIDES] = {2 + turns(0, 512) * (2.3 + (tiles[0] <= 512 ? 0.075 : 0.16) * stages(0)),
-                              3 + (tiles[1] <= 256 ? 2 + 0.25 * stages(1) : turns(1, 512) * (3 + 0.5 * stages(1))),
-                              tiles[2] <= 256 ? 7 + 0.46 * stages(2) : 4 + turns(2, 512) * (12 + 1.1 * stages(2)),
-                              turns(3, 256) * (12 + (tiles[3] <= 160 ? 0.68 : 0.83) * stages(3)),
-                              turns(4, 256) * (22 + (tiles[4] <= 160 ? 1.1 : 1.4) * stages(4))};
+  const double cost[kMuonKindsOf] = {2 + turns(0, 512) * (2.3 + (tiles[0] <= 512 ? 0.075 : 0.16) * stages(0)),
+                                     3 + (tiles[1] <= 256 ? 2 + 0.25 * stages(1) : turns(1, 512) * (3 + 0.5 * stages(1))),
+                                     tiles[2] <= 256 ? 8 + 0.46 * stages(2) : 4 + turns(2, 512) * (12 + 1.1 * stages(2)),
+                                     turns(3, 256) * (12 + (tiles[3] <= 160 ? 0.68 : 0.83) * stages(3)),
+                                     turns(4, 256) * (22 + (tiles[4] <= 160 ? 1.1 : 1.4) * stages(4)),
+                                     tiles[5] <= 256 ? 5 + 0.47 * stages(5) : 4 + turns(5, 512) * (2.5 + 0.7 * stages(5)),
+                                     turns(6, 256) * (12 + 0.87 * stages(6))};
+  // (Tiles of symmetric results are squares; those of 256 have no registers left for what the second product reads as well.)
+  constexpr int KINDS = MODE == kMuonPoly ? 4 : MODE == kMuonGram ? 5 : kMuonKindsOf;
   int best = 0;
-  for (int t = 1; t < (MODE == kMuonPoly ? SIDES - 1 : SIDES); ++t)            // (tiles of 256 have no registers left for what the second product reads as well)
+  for (int t = 1; t < KINDS; ++t)
     if (cost[t] < cost[best]) best = t;
   if (best == 0) {
-    count_muon_tiles<MODE>(a, 32);
+    count_muon_tiles<MODE>(a, 32, 32);
     hipLaunchKernelGGL((muon_small_kernel<2, MODE>), dim3(a.count), dim3(256), 0, stream, a);
   } else if (best == 1) {
-    launch_muon_tiles<1, 4, MODE>(a, stream);
+    launch_muon_tiles<1, 1, 4, MODE>(a, stream);
   } else if (best == 2) {
     // Where every CU has one tile at most, a third stage lies in LDS instead of a second workgroup's (X X^T of six matrices of 1024 x 4096 in two parts, 216 tiles, 95 us, 126 by two;
     // of 4096 x 8192, 528 tiles, 181 by two).
-    if (tiles[2] <= 256) launch_muon_tiles<2, 3, MODE>(a, stream);
-    else launch_muon_tiles<2, 2, MODE>(a, stream);
+    if (tiles[2] <= 256) launch_muon_tiles<2, 2, 3, MODE>(a, stream);
+    else launch_muon_tiles<2, 2, 2, MODE>(a, stream);
   } else if (best == 3) {
-    launch_muon_tiles<3, 3, MODE>(a, stream);
-  } else if constexpr (MODE != kMuonPoly) {
-    launch_muon_tiles<4, 2, MODE>(a, stream);
+    launch_muon_tiles<3, 3, 3, MODE>(a, stream);
+  } else if constexpr (KINDS > 4) {
+    if (best == 4) launch_muon_tiles<4, 4, 2, MODE>(a, stream);
+    else if constexpr (KINDS > 5) {
+      if (best == 5) launch_muon_tiles<1, 2, 3, MODE>(a, stream);
+      else launch_muon_tiles<2, 4, 3, MODE>(a, stream);
+    }
   }
 }
 

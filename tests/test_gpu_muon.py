@@ -72,9 +72,10 @@ def test_directions(rows, cols, wide):
     assert np.array_equal(values(parts_of(state, [(rows, cols)])[0]), values(grad))
 
 
-# (rows, columns, matrices): between them, each of the three products goes by tiles of 32, 64, 128, 192 and 256 (the second one not by 256), whole and cut ones, several to a workgroup
+# (rows, columns, matrices): between them, each of the three products goes by tiles of 32, 64, 128, 192 and 256 (the second one not by 256; the third one by 64 x 128 and 128 x 256, too), whole
+# and cut ones, several to a workgroup
 LARGE = [(256, 512, 24, False), (333, 1531, 3, True), (700, 2100, 2, True), (1000, 1900, 6, False), (1024, 4096, 6, True), (2100, 3000, 1, False), (2050, 4100, 2, False), (4000, 4100, 1, False), (1536, 1536, 5, True),
-         (4500, 2300, 3, False)]
+         (4500, 2300, 3, False), (130, 60, 400, False), (1000, 4000, 3, True)]
 
 
 @pytest.mark.parametrize("rows,cols,count,wide", LARGE)
