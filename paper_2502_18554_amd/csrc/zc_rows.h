@@ -36,24 +36,36 @@ __device__ inline RawEight<WIDE> load_eight(const void* base, u64 at, i32 left) 
     const bool four = left & 4, two = left & 2, one = left & 1;
     if constexpr (WIDE) {
       const u32* const from = static_cast<const u32*>(base) + at;
-      const W4At a = four ? *reinterpret_cast<const W4At*>(from) : W4At{};
-      const W2At b = two ? *reinterpret_cast<const W2At*>(from + (left & 4)) : W2At{};
-      const u32 c = one ? from[left & 6] : 0u;
-      const u32 n0 = two ? b.w[0] : c, n1 = b.w[1], n2 = two ? c : 0u;
-      r.w[0] = four ? a.w[0] : n0;
-      r.w[1] = four ? a.w[1] : n1;
-      r.w[2] = four ? a.w[2] : n2;
-      r.w[3] = a.w[3];
+      u32 a0 = 0, a1 = 0, a2 = 0, a3 = 0, b0 = 0, b1 = 0, c = 0;
+      if (four) {
+        const W4At v = *reinterpret_cast<const W4At*>(from);
+        a0 = v.w[0], a1 = v.w[1], a2 = v.w[2], a3 = v.w[3];
+      }
+      if (two) {
+        const W2At v = *reinterpret_cast<const W2At*>(from + (left & 4));
+        b0 = v.w[0], b1 = v.w[1];
+      }
+      if (one) c = from[left & 6];
+      const u32 n0 = two ? b0 : c, n1 = b1, n2 = two ? c : 0u;
+      r.w[0] = four ? a0 : n0;
+      r.w[1] = four ? a1 : n1;
+      r.w[2] = four ? a2 : n2;
+      r.w[3] = a3;
       r.w[4] = four ? n0 : 0u;
       r.w[5] = four ? n1 : 0u;
       r.w[6] = four ? n2 : 0u;
     } else {
       const u16* const from = static_cast<const u16*>(base) + at;
-      const H4At a = four ? *reinterpret_cast<const H4At*>(from) : H4At{};
-      const u32 b = two ? reinterpret_cast<const H2At*>(from + (left & 4))->w : 0u, c = one ? u32(from[left & 6]) : 0u;
+      u32 a0 = 0, a1 = 0, b = 0, c = 0;
+      if (four) {
+        const H4At v = *reinterpret_cast<const H4At*>(from);
+        a0 = v.w[0], a1 = v.w[1];
+      }
+      if (two) b = reinterpret_cast<const H2At*>(from + (left & 4))->w;
+      if (one) c = from[left & 6];
       const u32 n0 = two ? b : c, n1 = two ? c : 0u;
-      r.w[0] = four ? a.w[0] : n0;
-      r.w[1] = four ? a.w[1] : n1;
+      r.w[0] = four ? a0 : n0;
+      r.w[1] = four ? a1 : n1;
       r.w[2] = four ? n0 : 0u;
       r.w[3] = four ? n1 : 0u;
     }
@@ -119,15 +131,23 @@ __device__ inline void store_raw_eight(void* base, u64 at, i32 left, const RawEi
     if constexpr (WIDE) {
       u32* const to = static_cast<u32*>(base) + at;
       if (four) *reinterpret_cast<W4At*>(to) = W4At{{r.w[0], r.w[1], r.w[2], r.w[3]}};
-      const u32 n0 = four ? r.w[4] : r.w[0], n1 = four ? r.w[5] : r.w[1], n2 = four ? r.w[6] : r.w[2];
-      if (two) *reinterpret_cast<W2At*>(to + (left & 4)) = W2At{{n0, n1}};
-      if (left & 1) to[left & 6] = two ? n2 : n0;
+      u32 n0 = r.w[0], n1 = r.w[1], n2 = r.w[2];
+      if (four) n0 = r.w[4], n1 = r.w[5], n2 = r.w[6];
+      if (two) {
+        *reinterpret_cast<W2At*>(to + (left & 4)) = W2At{{n0, n1}};
+        n0 = n2;
+      }
+      if (left & 1) to[left & 6] = n0;
     } else {
       u16* const to = static_cast<u16*>(base) + at;
       if (four) *reinterpret_cast<H4At*>(to) = H4At{{r.w[0], r.w[1]}};
-      const u32 n0 = four ? r.w[2] : r.w[0], n1 = four ? r.w[3] : r.w[1];
-      if (two) reinterpret_cast<H2At*>(to + (left & 4))->w = n0;
-      if (left & 1) to[left & 6] = u16(two ? n1 : n0);
+      u32 n0 = r.w[0], n1 = r.w[1];
+      if (four) n0 = r.w[2], n1 = r.w[3];
+      if (two) {
+        reinterpret_cast<H2At*>(to + (left & 4))->w = n0;
+        n0 = n1;
+      }
+      if (left & 1) to[left & 6] = u16(n0);
     }
   }
 }
