@@ -284,7 +284,9 @@ int zc_embedding(const void* d_table, int table_type, size_t table_rows, size_t 
   EmbeddingArgs a{d_table, d_tokens, d_out, n, table_rows, cols, table_stride, out_stride, float(scale), table_type, out_type, 4};
   while (a.pieces_log2 < 8 && (u64(8) << a.pieces_log2) < cols) ++a.pieces_log2;
   const u64 at_once = u64(256) >> a.pieces_log2, across = (cols + (u64(8) << a.pieces_log2) - 1) / (u64(8) << a.pieces_log2);
-  const dim3 grid(at_most((n + at_once - 1) / at_once, 1 << 20), at_most(across, 1 << 12));
+  // As many workgroups as rows where they are few, of up to four rows each where the GPU is full.
+  const u64 groups = (n + at_once - 1) / at_once, full = groups * across > 4096 ? (groups + kEmbeddingRows - 1) / kEmbeddingRows : groups;
+  const dim3 grid(at_most(full, 1 << 20), at_most(across, 1 << 12));
   if (token_bits == 32) launch_embedding<32>(a, grid, static_cast<hipStream_t>(hip_stream));
   else launch_embedding<64>(a, grid, static_cast<hipStream_t>(hip_stream));
   return launched();

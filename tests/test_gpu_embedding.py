@@ -45,6 +45,38 @@ def test_lookup(rows, cols, n, kinds, bits):
     assert torch.equal(out, want) and bool((room[:, cols:] == -7).all())
 
 
+def test_far_rows():
+    """Tables whose last rows lie more than 2^32 bytes behind their first ones, read and added to."""
+    rows, cols = 300000, 8192
+    table = torch.zeros(rows, cols, dtype=torch.bfloat16, device=DEV)
+    at = torch.tensor([rows - 1, 0, rows // 2, rows - 1, rows - 7, 262144, rows], device=DEV)
+    g = generator(1)
+    table[at[:-1]] = torch.randn(6, cols, generator=g, device=DEV).bfloat16()
+    out = torch.empty(7, cols, dtype=torch.bfloat16, device=DEV)
+    assert zc.zc_embedding(table, at, out) == 0
+    assert torch.equal(out[:-1], table[at[:-1]]) and bool((out[-1] == 0).all())
+    dy = torch.randint(-3, 4, (7, cols), generator=g, device=DEV).float()
+    table[at[:-1]] = 1.0
+    assert zc.zc_embedding_backward(dy, at, table, workspace(7, rows, cols), add=True) == 0
+    want = 1 + dy[:-1]
+    want[0] = want[3] = 1 + dy[0] + dy[3]
+    assert torch.equal(table[at[:-1]].float(), want)
+    table.zero_()
+    assert zc.zc_embedding_backward(dy, at, table, workspace(7, rows, cols)) == 0
+    assert torch.equal(table[at[:-1]].float(), want - 1) and int((table != 0).any(dim=1).sum()) == 5
+
+
+def test_many_tokens():
+    """More rows than workgroups, each of which takes several."""
+    g = generator(9)
+    for n, cols in ((40000, 24), (9001, 520), (5000, 4100)):
+        table = torch.randn(977, cols, generator=g, device=DEV)
+        tokens = torch.randint(-1, 977, (n,), generator=g, device=DEV, dtype=torch.int32)
+        out = torch.full((n + 1, cols), -7.0, dtype=torch.float16, device=DEV)
+        assert zc.zc_embedding(table, tokens, out[:n], scale=0.5) == 0
+        assert torch.equal(out[:n], torch.where((tokens >= 0)[:, None], table[tokens.clamp(min=0).long()] * 0.5, 0).half()) and bool((out[n] == -7).all())
+
+
 def check_gradient(dy, tokens, grad, before, scale, kind):
     want, size, count = model.embedding_backward(values(dy), tokens.cpu().numpy().reshape(-1), grad.shape[0], float(np.float32(scale)))
     if before is not None:

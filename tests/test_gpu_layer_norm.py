@@ -116,10 +116,28 @@ def test_in_place(cols):
     dy, _ = matrix(700, cols, "bf16", g)
     dx, dw, ws = torch.empty_like(x), torch.empty(cols, device=DEV), workspace(700, cols)
     assert zc.zc_layer_norm_backward(dy, x, stats, w, dx, dw, None, ws) == 0
-    for of in (dy.clone(), x.clone()):
-        again, over = torch.empty(cols, device=DEV), of
-        assert zc.zc_layer_norm_backward(over if of is not x and torch.equal(of, dy) else dy, over if torch.equal(of, x) else x, stats, w, over, again, None, ws) == 0
-        assert torch.equal(over, dx) and torch.equal(again, dw)
+    over, again = dy.clone(), torch.empty(cols, device=DEV)
+    assert zc.zc_layer_norm_backward(over, x, stats, w, over, again, None, ws) == 0
+    assert torch.equal(over, dx) and torch.equal(again, dw)
+    over = x.clone()
+    assert zc.zc_layer_norm_backward(dy, over, stats, w, over, again, None, ws) == 0
+    assert torch.equal(over, dx) and torch.equal(again, dw)
+
+
+def test_far_rows():
+    """Rows that lie more than 2^32 values apart in all."""
+    rows, cols, apart = 70000, 40, 65000
+    room = torch.empty(rows * apart, dtype=torch.bfloat16, device=DEV)
+    x = room.view(rows, apart)[:, :cols]
+    x.copy_(torch.randn(rows, cols, generator=generator(2), device=DEV))
+    near, out, stats, near_stats = x.contiguous(), torch.empty(rows, cols, device=DEV), torch.empty(2, rows, device=DEV), torch.empty(2, rows, device=DEV)
+    want = torch.empty_like(out)
+    assert zc.zc_layer_norm(near, None, None, want, near_stats) == 0 and zc.zc_layer_norm(x, None, None, out, stats) == 0
+    assert torch.equal(out, want) and torch.equal(stats, near_stats)
+    ws, dw, again, near_dx = workspace(rows, cols), torch.empty(cols, device=DEV), torch.empty(cols, device=DEV), torch.empty_like(near)
+    assert zc.zc_layer_norm_backward(want, near, stats, None, near_dx, dw, None, ws) == 0
+    assert zc.zc_layer_norm_backward(want, x, stats, None, x, again, None, ws) == 0
+    assert torch.equal(x, near_dx) and torch.equal(dw, again)
 
 
 def test_large_mean_and_constant_rows():

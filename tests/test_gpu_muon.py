@@ -56,7 +56,7 @@ def allowed(u, iterations, wide, device="cpu"):
     return 1.5 * off(model.orthogonalised(u, iterations, 2 if wide else 1, device), exact) + 2.0 ** -17
 
 
-SHAPES = [(1, 1), (1, 7), (5, 3), (17, 17), (40, 30), (64, 64), (65, 130), (128, 128), (129, 257), (300, 100), (256, 512), (513, 700), (1100, 1300), (1290, 1030), (96, 4000)]
+SHAPES = [(1, 1), (1, 7), (5, 3), (17, 17), (40, 30), (64, 64), (65, 130), (128, 128), (129, 257), (300, 100), (256, 512), (513, 700), (1100, 1300), (1290, 1030), (96, 4000), (2, 70001), (50001, 3)]
 
 
 @pytest.mark.parametrize("rows,cols", SHAPES)
