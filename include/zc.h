@@ -380,13 +380,13 @@ int zc_mx_linear(const void* d_x, int x_type, size_t x_stride, const void* d_w, 
  *   mean = sum x / cols;  d = 1 / sqrt(sum (x - mean)^2 / cols + eps);  out = (x - mean) d w + b
  * rounded once, to out_type.  d_w, d_b: cols values of w_type each, either may be NULL (1 and 0).  d_stats (may be NULL): 2 rows binary32 values, the
  * rows' means, then their d, for the backward pass.  d_out may be d_x, of the same type and stride.
- * A row with a value that is not finite becomes NaNs.  rows below 2^31, cols up to 2^27.  Errors: ARG, HIP. */
+ * A row with a value that is not finite becomes NaNs, here and in the gradients.  rows below 2^31, cols up to 2^27.  Errors: ARG (also eps negative or not finite in binary32), HIP. */
 int zc_layer_norm(const void* d_x, int x_type, size_t rows, size_t cols, size_t x_stride, const void* d_w, const void* d_b, int w_type, double eps,
                   void* d_out, int out_type, size_t out_stride, float* d_stats, void* hip_stream);
 
 /* Its gradients, from that of its output, d_dy.  With z = (x - mean) d and h = dy w:
  *   dx = d (h - sum h / cols - z sum (h z) / cols);  dw = sum over the rows of dy z;  db = sum over the rows of dy
- * d_dx, d_dw, d_db: any may be NULL.  ZC_ADD: dx is added to what d_dx holds (the gradient of a residual stream); ZC_ADD_WEIGHTS: dw and db
+ * d_dx, d_dw, d_db: any may be NULL; d_dw and d_db are not the same.  ZC_ADD: dx is added to what d_dx holds (the gradient of a residual stream); ZC_ADD_WEIGHTS: dw and db
  * likewise.  d_dx may be d_dy or d_x, of the same type and stride.  Sums in binary32, results rounded once; their order depends on the sizes only, so that
  * equal calls give equal results.  No rows: dw and db are zeros.  d_ws: 16-byte aligned, its content irrelevant, one for calls that may overlap. */
 size_t zc_layer_norm_workspace_bytes(size_t rows, size_t cols);
@@ -394,14 +394,15 @@ int zc_layer_norm_backward(const void* d_dy, int dy_type, size_t dy_stride, cons
                            int w_type, size_t rows, size_t cols, void* d_dx, int dx_type, size_t dx_stride, void* d_dw, void* d_db, int dw_type, unsigned flags,
                            void* d_ws, size_t ws_bytes, void* hip_stream);
 
-/* Rows of a table by tokens: out[i] = scale x table[token[i]], rounded once; zeros where token[i] is not in [0, table_rows), as padding is.  d_tokens: n whole numbers with sign, of
- * token_bits 32 or 64.  Up to 2^29 rows of up to 2^23 values; n below 2^31.  Errors: ARG, HIP. */
+/* Rows of a table by tokens: out[i] = scale x table[token[i]], a product in binary32 (exact for scale 1), then rounded to out_type; zeros where token[i] is not in [0, table_rows), as
+ * padding is.  d_out does not overlap d_table.  d_tokens: n whole numbers with sign, of token_bits 32 or 64.  Up to 2^29 rows of up to 2^23 values; n below 2^31.  Errors: ARG (also a scale that is not finite in binary32), HIP. */
 int zc_embedding(const void* d_table, int table_type, size_t table_rows, size_t cols, size_t table_stride, const void* d_tokens, int token_bits, size_t n, double scale,
                  void* d_out, int out_type, size_t out_stride, void* hip_stream);
 
 /* The table's gradient from that of the output, d_dy (n x cols): grad[v] = scale x the sum of dy[i] over all i with token[i] = v, zeros for a row that no token
  * names.  ZC_ADD: added to what d_grad holds; rows that no token names stay as they are.  Sums in binary32, rounded once; their order depends on the sizes and
- * the tokens only, so that equal calls give equal results.  d_ws: 16-byte aligned, its content irrelevant, one for calls that may overlap. */
+ * the tokens only, so that equal calls give equal results.  d_ws: 16-byte aligned, its content irrelevant, one for calls that may overlap.
+ * The tokens are read by table_rows / 1024 workgroups (256 at least), all of them by each. */
 size_t zc_embedding_workspace_bytes(size_t n, size_t table_rows, size_t cols);
 int zc_embedding_backward(const void* d_dy, int dy_type, size_t dy_stride, const void* d_tokens, int token_bits, size_t n, double scale, void* d_grad, int grad_type,
                           size_t table_rows, size_t cols, size_t grad_stride, unsigned flags, void* d_ws, size_t ws_bytes, void* hip_stream);
@@ -413,9 +414,9 @@ int zc_embedding_backward(const void* d_dy, int dy_type, size_t dy_stride, const
  *   p' = p (1 - lr weight_decay) - lr factor X
  * factor: sqrt(max(1, rows / cols)); with ZC_MUON_MATCH_RMS 0.2 sqrt(max(rows, cols)).
  * The products' operands are X, A and B rounded to 11 bits (binary16, scaled by 2^12), with ZC_MUON_WIDE to 22 bits (two of them; three times the work), sums are in
- * binary32: p' is off by at most some 2^-9, 2^-18 with ZC_MUON_WIDE, of lr factor times a typical value of X.
+ * binary32: p' is off by some 2^-9, with ZC_MUON_WIDE 2^-18, of lr factor times a typical value of X.
  * param_type, grad_type, d_copies, copy_type, d_grad_scale: as in zc_adamw (a scale that is not finite: nothing changes).  A gradient with a value that is not finite makes its
- * matrix's p' and what it touches of m' NaNs.  d_state: zc_muon_state_bytes bytes, 16-byte aligned, zeros before the first step: m of all matrices in their order as binary32 values, each
+ * matrix's p' and what it touches of m' NaNs.  No two results are the same memory.  d_state: zc_muon_state_bytes bytes, 16-byte aligned, zeros before the first step: m of all matrices in their order as binary32 values, each
  * filled up to a multiple of 32 of them.  d_ws: zc_muon_workspace_bytes bytes, 256-byte aligned, its content irrelevant, one for calls that may overlap.  Equal calls
  * give equal results.  Up to 2^20 rows and columns, 1 to 100 iterations.  Errors: ARG, HIP. */
 #define ZC_MUON_NESTEROV 1u

@@ -124,6 +124,22 @@ u64 muon_workspace(int k, const size_t* rows, const size_t* cols, u32 planes) {
   return most;
 }
 
+// Whether two of a call's results begin at one place: launches take many matrices together, so that one would be lost.
+bool share_results(int k, const size_t* rows, const size_t* cols, void* const* params, void* const* copies) {
+  for (int i = 0; i < k; ++i) {
+    if (rows[i] == 0 || cols[i] == 0) continue;
+    const void *const p = params[i], *const c = copies ? copies[i] : nullptr;
+    bool twice = p == c;
+    for (int j = 0; j < i; ++j) {
+      const bool there = rows[j] != 0 && cols[j] != 0;
+      const void *const of = params[j], *const copy = copies ? copies[j] : nullptr;
+      twice |= there && (of == p || of == c || (copy && (copy == p || copy == c)));
+    }
+    if (twice) return true;
+  }
+  return false;
+}
+
 u64 muon_tiles(const MuonTensor& t, int mode, u64 high, u64 wide) {
   const u64 down = (t.r + high - 1) / high, across = (t.c + wide - 1) / wide;
   return mode == kMuonGram || mode == kMuonPoly ? down * (down + 1) / 2 : down * across;
@@ -218,7 +234,7 @@ int zc_layer_norm(const void* d_x, int x_type, size_t rows, size_t cols, size_t 
                   void* d_out, int out_type, size_t out_stride, float* d_stats, void* hip_stream) {
   if (!norm_sizes_valid(rows, cols) || !matrix_valid(d_x, x_type, rows, cols, x_stride) || !matrix_valid(d_out, out_type, rows, cols, out_stride)) return ZC_ERR_ARG;
   if (!type_valid(w_type) || !aligned(d_w, value_bytes(w_type)) || !aligned(d_b, value_bytes(w_type)) || !aligned(d_stats, 4)) return ZC_ERR_ARG;
-  if (!(std::isfinite(eps) && eps >= 0) || !same_or_apart(d_out, out_type, out_stride, d_x, x_type, x_stride)) return ZC_ERR_ARG;
+  if (!(std::isfinite(float(eps)) && eps >= 0) || !same_or_apart(d_out, out_type, out_stride, d_x, x_type, x_stride)) return ZC_ERR_ARG;
   if (rows == 0 || cols == 0) return ZC_OK;
   const NormArgs a{d_x, d_w, d_b, d_out, d_stats, rows, cols, x_stride, out_stride, float(eps), x_type, w_type, out_type};
   const auto stream = static_cast<hipStream_t>(hip_stream);
@@ -246,6 +262,7 @@ int zc_layer_norm_backward(const void* d_dy, int dy_type, size_t dy_stride, cons
   if (d_dx && (!matrix_valid(d_dx, dx_type, rows, cols, dx_stride) || !same_or_apart(d_dx, dx_type, dx_stride, d_dy, dy_type, dy_stride) ||
                !same_or_apart(d_dx, dx_type, dx_stride, d_x, x_type, x_stride)))
     return ZC_ERR_ARG;
+  if (d_dw && d_dw == d_db) return ZC_ERR_ARG;
   if ((rows && cols && !d_stats) || ws_bytes < norm_workspace(rows, cols) || (rows && cols && !d_ws)) return ZC_ERR_ARG;
   const bool sums = d_dw || d_db;
   if (cols == 0 || (!sums && (rows == 0 || !d_dx))) return ZC_OK;
@@ -279,7 +296,7 @@ int zc_layer_norm_backward(const void* d_dy, int dy_type, size_t dy_stride, cons
 int zc_embedding(const void* d_table, int table_type, size_t table_rows, size_t cols, size_t table_stride, const void* d_tokens, int token_bits, size_t n, double scale,
                  void* d_out, int out_type, size_t out_stride, void* hip_stream) {
   if (!table_valid(table_rows, cols, n, token_bits) || !matrix_valid(d_table, table_type, table_rows, cols, table_stride) || !matrix_valid(d_out, out_type, n, cols, out_stride)) return ZC_ERR_ARG;
-  if (!std::isfinite(scale) || (n && !d_tokens) || !aligned(d_tokens, u64(token_bits / 8))) return ZC_ERR_ARG;
+  if (!std::isfinite(float(scale)) || (n && !d_tokens) || !aligned(d_tokens, u64(token_bits / 8))) return ZC_ERR_ARG;
   if (n == 0 || cols == 0) return ZC_OK;
   EmbeddingArgs a{d_table, d_tokens, d_out, n, table_rows, cols, table_stride, out_stride, float(scale), table_type, out_type, 4};
   while (a.pieces_log2 < 8 && (u64(8) << a.pieces_log2) < cols) ++a.pieces_log2;
@@ -297,7 +314,7 @@ size_t zc_embedding_workspace_bytes(size_t n, size_t table_rows, size_t cols) { 
 int zc_embedding_backward(const void* d_dy, int dy_type, size_t dy_stride, const void* d_tokens, int token_bits, size_t n, double scale, void* d_grad, int grad_type,
                           size_t table_rows, size_t cols, size_t grad_stride, unsigned flags, void* d_ws, size_t ws_bytes, void* hip_stream) {
   if (!table_valid(table_rows, cols, n, token_bits) || !matrix_valid(d_dy, dy_type, n, cols, dy_stride) || !matrix_valid(d_grad, grad_type, table_rows, cols, grad_stride)) return ZC_ERR_ARG;
-  if (!std::isfinite(scale) || (n && !d_tokens) || !aligned(d_tokens, u64(token_bits / 8)) || (flags & ~ZC_ADD) || !aligned(d_ws, 16)) return ZC_ERR_ARG;
+  if (!std::isfinite(float(scale)) || (n && !d_tokens) || !aligned(d_tokens, u64(token_bits / 8)) || (flags & ~ZC_ADD) || !aligned(d_ws, 16)) return ZC_ERR_ARG;
   const TokenPlan plan(n, table_rows, cols);
   if (ws_bytes < plan.bytes || !d_ws) return ZC_ERR_ARG;
   const bool add = flags & ZC_ADD;
@@ -346,6 +363,7 @@ int zc_muon(int k, const size_t* rows, const size_t* cols, void* const* d_params
     if (!d_params[i] || !d_grads[i] || !aligned(d_params[i], value_bytes(param_type)) || !aligned(d_grads[i], value_bytes(grad_type))) return ZC_ERR_ARG;
     if (d_copies && !aligned(d_copies[i], value_bytes(copy_type))) return ZC_ERR_ARG;
   }
+  if (share_results(k, rows, cols, d_params, d_copies)) return ZC_ERR_ARG;
   const auto stream = static_cast<hipStream_t>(hip_stream);
   float* m = static_cast<float*>(d_state);
   for (int i = 0; i < k;) {

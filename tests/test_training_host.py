@@ -47,13 +47,13 @@ def test_sizes(L):
 
 def test_refusals_of_the_norm(L):
     f = caller(L.zc_layer_norm, x=A, xt=1, rows=8, cols=64, xs=64, w=B, b=B, wt=0, eps=1e-5, out=D, ot=1, os=64, stats=E, stream=None)
-    for bad in (dict(x=None), dict(x=A + 1), dict(xt=3), dict(xs=63), dict(w=B + 2), dict(b=B + 1), dict(wt=-1), dict(eps=-1.0), dict(eps=NAN), dict(eps=INF), dict(out=None), dict(out=D + 1),
+    for bad in (dict(x=None), dict(x=A + 1), dict(xt=3), dict(xs=63), dict(w=B + 2), dict(b=B + 1), dict(wt=-1), dict(eps=-1.0), dict(eps=NAN), dict(eps=INF), dict(eps=1e39), dict(out=None), dict(out=D + 1),
                 dict(ot=7), dict(os=10), dict(stats=E + 2), dict(rows=1 << 31), dict(cols=(1 << 27) + 1, xs=1 << 28, os=1 << 28), dict(out=A, ot=2), dict(out=A, os=65)):
         assert f(**bad) == ARG, bad
     assert f(rows=0) == OK and f(cols=0, xs=0, os=0) == OK and f(rows=0, x=None, out=None) == OK
-    g = caller(L.zc_layer_norm_backward, dy=A, dyt=1, dys=64, x=B, xt=0, xs=64, stats=E, w=D, wt=0, rows=8, cols=64, dx=D, dxt=0, dxs=64, dw=E, db=E, dwt=0, flags=3, ws=A, bytes=1 << 20, stream=None)
+    g = caller(L.zc_layer_norm_backward, dy=A, dyt=1, dys=64, x=B, xt=0, xs=64, stats=E, w=D, wt=0, rows=8, cols=64, dx=D, dxt=0, dxs=64, dw=E, db=E + 4096, dwt=0, flags=3, ws=A, bytes=1 << 20, stream=None)
     for bad in (dict(dy=None), dict(dy=A + 1), dict(dyt=4), dict(dys=63), dict(x=None), dict(x=B + 2), dict(xt=9), dict(xs=0), dict(stats=None), dict(stats=E + 1), dict(w=D + 2), dict(wt=3),
-                dict(rows=1 << 31), dict(dx=D + 2), dict(dxt=5), dict(dxs=63), dict(dw=E + 2), dict(db=E + 1), dict(dwt=-1), dict(flags=4), dict(ws=None), dict(ws=A + 8), dict(bytes=8 * 64 - 1),
+                dict(rows=1 << 31), dict(dx=D + 2), dict(dxt=5), dict(dxs=63), dict(dw=E + 2), dict(db=E + 1), dict(db=E), dict(dwt=-1), dict(flags=4), dict(ws=None), dict(ws=A + 8), dict(bytes=8 * 64 - 1),
                 dict(dx=A, dxt=0), dict(dx=A, dxt=1, dxs=65), dict(dx=B, dxs=80)):
         assert g(**bad) == ARG, bad
     assert g(cols=0, dys=0, xs=0, dxs=0) == OK and g(rows=0, dw=None, db=None) == OK
@@ -62,11 +62,11 @@ def test_refusals_of_the_norm(L):
 def test_refusals_of_the_embedding(L):
     f = caller(L.zc_embedding, table=A, tt=1, rows=100, cols=64, stride=64, tokens=B, bits=64, n=8, scale=1.0, out=D, ot=0, os=64, stream=None)
     for bad in (dict(table=None), dict(table=A + 1), dict(tt=3), dict(stride=63), dict(rows=(1 << 29) + 1), dict(cols=(1 << 23) + 1, stride=1 << 24, os=1 << 24), dict(tokens=None), dict(tokens=B + 4),
-                dict(tokens=B + 2, bits=32), dict(bits=16), dict(n=1 << 31), dict(scale=NAN), dict(scale=INF), dict(out=None), dict(out=D + 2), dict(ot=8), dict(os=63)):
+                dict(tokens=B + 2, bits=32), dict(bits=16), dict(n=1 << 31), dict(scale=NAN), dict(scale=INF), dict(scale=-1e39), dict(out=None), dict(out=D + 2), dict(ot=8), dict(os=63)):
         assert f(**bad) == ARG, bad
     assert f(n=0) == OK and f(cols=0, stride=0, os=0) == OK
     g = caller(L.zc_embedding_backward, dy=A, dyt=1, dys=64, tokens=B, bits=32, n=8, scale=1.0, grad=D, gt=0, rows=100, cols=64, stride=64, flags=1, ws=E, bytes=1 << 20, stream=None)
-    for bad in (dict(dy=None), dict(dy=A + 1), dict(dyt=3), dict(dys=63), dict(tokens=None), dict(tokens=B + 2), dict(bits=8), dict(n=1 << 31), dict(scale=-INF), dict(grad=None), dict(grad=D + 2),
+    for bad in (dict(dy=None), dict(dy=A + 1), dict(dyt=3), dict(dys=63), dict(tokens=None), dict(tokens=B + 2), dict(bits=8), dict(n=1 << 31), dict(scale=-INF), dict(scale=1e300), dict(grad=None), dict(grad=D + 2),
                 dict(gt=3), dict(rows=(1 << 29) + 1), dict(stride=1), dict(flags=2), dict(ws=None), dict(ws=E + 4), dict(bytes=100)):
         assert g(**bad) == ARG, bad
     assert g(n=0) == OK and g(rows=0) == OK and g(cols=0, dys=0, stride=0) == OK
@@ -79,6 +79,10 @@ def test_refusals_of_the_step_for_matrices(L):
                 dict(grads=words(0)), dict(params=words(A + 2)), dict(grads=words(B + 1)), dict(state=None), dict(state=D + 8), dict(bytes=4 * 320 - 1), dict(lr=-1.0), dict(lr=NAN), dict(lr=INF), dict(mu=1.0),
                 dict(mu=-0.1), dict(mu=NAN), dict(wd=-1.0), dict(wd=INF), dict(n=0), dict(n=101), dict(flags=8), dict(scale=D + 2), dict(ws=None), dict(ws=0x100080), dict(wsb=4096), dict(rows=words((1 << 20) + 1))):
         assert f(**bad) == ARG, bad
+    twice = dict(k=2, rows=words(16, 8), cols=words(20, 5), grads=words(B, B), bytes=8 * 320)
+    for bad in (dict(params=words(A, A)), dict(params=words(A, D), copies=words(E, E)), dict(params=words(A, D), copies=words(D, 0)), dict(params=words(A, D), copies=words(0, A)),
+                dict(params=words(A, D), copies=words(A, 0))):
+        assert f(**twice, **bad) == ARG, bad
     assert f(k=0) == OK and f(rows=words(0), params=words(0), grads=words(0), state=None, bytes=0, ws=None, wsb=0) == OK
 
 
