@@ -22,6 +22,7 @@
 
 #include <utility>
 
+#include "zc_muon_ask.h"
 #include "zc_rows.h"
 
 namespace zc {
@@ -532,7 +533,8 @@ __global__ __launch_bounds__(256, muon_groups(TM, TN, S)) void muon_product_kern
   if (tiles.first >= tiles.end) return;
 
   // What is asked for next: a tile's rows, and how far along them.
-  u32 ask_tile = tiles.first, ask_stage = 0, ask_stages = 0, ask_segment = 0;
+  MuonAsked asked{tiles.first, 0, 0};
+  u32 ask_stages = 0;
   MuonRows rows_a, rows_b;
   const u32 my_row = tid / BLOCKS;
   // Which block of a row is where: the place's number exchanged by what tells the rows apart that are read together.
@@ -540,16 +542,16 @@ __global__ __launch_bounds__(256, muon_groups(TM, TN, S)) void muon_product_kern
   const auto key_b = [](u32 row) { return (row >> 1 & 1u) | (row >> 3 & 2u) | (row & 4u); };
   u32 mine_a[LOADS_A], mine_b[LOADS - LOADS_A];          // a thread's places in the tile's rows
   const auto aim = [&] {
-    const MuonOf of(a, ask_tile);
+    const MuonOf of(a, asked.tile);
     const u32 r = of.r, c = of.c;
     const MuonParts parts(r, c, a.planes);
     u32 row, col;
     const u32 down = (r + RA - 1) / RA, across = TRIANGLE ? down : (c + RB - 1) / RB;
-    MuonTiles<MODE>::place(ask_tile - of.first, down, across, row, col);
+    MuonTiles<MODE>::place(asked.tile - of.first, down, across, row, col);
     const u8* const at = of.at;
     const u64 plane_a = MODE == kMuonGram ? parts.plane_x : parts.plane_a, plane_b = MODE == kMuonGram ? parts.plane_x : MODE == kMuonPoly ? parts.plane_a : parts.plane_t;
-    const u8* const from_a = at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : parts.b) + (ask_segment == 2 ? plane_a : 0);
-    const u8* const from_b = at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : a.which ? parts.t1 : parts.t0) + (ask_segment == 1 ? plane_b : 0);
+    const u8* const from_a = at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : parts.b) + (asked.segment == 2 ? plane_a : 0);
+    const u8* const from_b = at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : a.which ? parts.t1 : parts.t0) + (asked.segment == 1 ? plane_b : 0);
     const u64 along = MODE == kMuonGram ? parts.row_x : parts.row_t;
     rows_a.aim(from_a, u64(row) * RA, r, 2 * along, RA);
     rows_b.aim(from_b, u64(col) * RB, TRIANGLE ? r : c, 2 * along, RB);
@@ -566,16 +568,9 @@ __global__ __launch_bounds__(256, muon_groups(TM, TN, S)) void muon_product_kern
   const auto next_stage = [&] {
     rows_a.move_on(ROW);
     rows_b.move_on(ROW);
-    if (++ask_stage < ask_stages) return;
-    ask_stage = 0;
-    if (a.planes > 1 && ++ask_segment < 3) {
-      aim();
-      return;
-    }
-    ask_segment = 0;
-    ask_tile += tiles.step;
-    if (ask_tile < tiles.end) aim();
-    else rows_a.bytes = rows_b.bytes = 0;
+    const MuonNext next = asked.next(ask_stages, a.planes, tiles.step, tiles.end);
+    if (next == MuonNext::kAim) aim();
+    else if (next == MuonNext::kNothing) rows_a.bytes = rows_b.bytes = 0;
   };
   const u32 lds0 = u32(reinterpret_cast<uintptr_t>((LdsWord*)&memory[0]));
   const auto ask = [&](u32 place, u32 i) {           // place: of the stage in LDS, in bytes

@@ -1,5 +1,7 @@
 """CPU tests of the host side of layer norm, embedding and the step for matrices: sizes, refusals that need no GPU, the native calls' choice of way."""
 import ctypes as C
+import os
+import subprocess
 
 import pytest
 import torch
@@ -110,3 +112,11 @@ def test_native_calls_leave_what_is_not_plain():
     b._native_layers.setup_training(*calls)
     for name, count in (("layer_norm", 7), ("layer_norm_backward", 11), ("embedding", 5), ("embedding_backward", 7), ("muon", 12)):
         assert getattr(b._native_layers, name)(*[None] * count) is NotImplemented and getattr(b._native_layers, name)() is NotImplemented
+
+
+def test_requests_end_with_the_last_tile(tmp_path):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "muon_ask_host")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", os.path.join(root, "tests", "host", "muon_ask_host.cpp"), "-o", exe], check=True)
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=60)
+    assert run.returncode == 0, run.stdout
