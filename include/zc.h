@@ -380,7 +380,7 @@ int zc_mx_linear(const void* d_x, int x_type, size_t x_stride, const void* d_w, 
  *   mean = sum x / cols;  d = 1 / sqrt(sum (x - mean)^2 / cols + eps);  out = (x - mean) d w + b
  * rounded once, to out_type.  d_w, d_b: cols values of w_type each, either may be NULL (1 and 0).  d_stats (may be NULL): 2 rows binary32 values, the
  * rows' means, then their d, for the backward pass.  d_out may be d_x, of the same type and stride.
- * A row with a value that is not finite becomes NaNs, here and in the gradients.  rows below 2^31, cols up to 2^27.  Errors: ARG (also eps negative or not finite in binary32), HIP. */
+ * A row with a value that is not finite becomes NaNs, here and in the gradients; of a finite row whose sum or sum of squares binary32 does not hold nothing is promised.  rows below 2^31, cols up to 2^27.  Errors: ARG (also eps negative or not finite in binary32), HIP. */
 int zc_layer_norm(const void* d_x, int x_type, size_t rows, size_t cols, size_t x_stride, const void* d_w, const void* d_b, int w_type, double eps,
                   void* d_out, int out_type, size_t out_stride, float* d_stats, void* hip_stream);
 

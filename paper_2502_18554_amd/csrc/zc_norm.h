@@ -5,7 +5,8 @@
 //
 // Bound by memory: a row is read once and stays in registers.  T lanes share a row, P pieces of eight values each.  The sums of a row need one exchange between
 // its waves: every wave makes the sum of its values and the squares around its own mean, and the waves' squares are brought to the row's mean by
-// sum (x - mean)^2 = sum over waves of [sum (x - mean_w)^2 + n_w (mean_w - mean)^2], which loses nothing where the mean is large against the deviations.
+// sum (x - mean)^2 = sum over waves of [sum (x - mean_w)^2 + n_w (mean_w - mean)^2], in which no large numbers are subtracted: what the means' own roundings leave in d, relative
+// to it, is no more than what they leave in (x - mean) d.
 // Workgroups take rows in turn and ask for the next one before they work on this one; weights stay in registers for all of them, and so do the backward pass's sums down
 // the columns, which a workgroup writes once.  A second launch adds the workgroups' sums in their order, so that equal calls give equal results.
 //
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(norm_threads<T>()) void norm_kernel(NormArgs a) {
       __syncthreads();
       const float2 of = of_wave < T / 64 ? exchange.slot[parity][of_wave] : make_float2(0.0f, 0.0f);
       mean = sum_of_16(of.x) * per_row;
-      const float off = of.x * per_its - mean;
+      const float off = its > 0.0f ? of.x * per_its - mean : 0.0f;       // (of a lane without a wave it would be the mean, whose square may pass binary32)
       squares = sum_of_16(__builtin_fmaf(off * off, its, of.y));
       parity ^= 1u;
     }
