@@ -5,7 +5,7 @@ import torch
 
 import paper_2502_18554_amd as zc
 import training_model as model
-from test_gpu_layer_norm import DEV, EPS, EPS32, check_forward, generator, matrix, values
+from test_gpu_layer_norm import DEV, EPS, EPS32, check_forward, generator, matrix, values, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +28,24 @@ def test_a_mean_whose_square_passes_binary32(cols, kind, mean, scale):
     e = 128 * model.U * size * d
     assert (np.abs(values(stats)[0] - want) <= 64 * model.U * size).all()
     assert (np.abs(values(stats)[1] - d) <= d * (64 * model.U + e + e * e / 2)).all()
+
+
+@pytest.mark.parametrize("cols", [7, 100, 300, 777, 1500, 2050, 5001, 8200, 12000, 20001])
+def test_gradients_of_constant_rows_of_large_values(cols):
+    """The mean times d, 6e38, is behind binary32's range, (x - mean) d is 0: lanes behind the row's end have to stay out of its sums.  Statistics are given, so that the
+    formula's gradients are those of the definition in 64 bits; tolerances as in test_gpu_layer_norm.py."""
+    g = generator(cols)
+    x, _ = matrix(5, cols, "f32", g)
+    x[1], x[4] = 2e36, -2e36
+    _, mean, d, _ = model.norm(values(x), np.ones(cols), np.zeros(cols), EPS32)
+    mean[[1, 4]], d[[1, 4]] = float(np.float32(2e36)) * np.array([1, -1]), EPS32 ** -0.5
+    stats = torch.tensor(np.stack([mean, d]), dtype=torch.float32, device=DEV)
+    w = torch.rand(cols, generator=g, device=DEV).add_(0.5)
+    dy, _ = matrix(5, cols, "f32", g)
+    dx, dw, db = torch.empty_like(x), torch.empty(cols, device=DEV), torch.empty(cols, device=DEV)
+    assert zc.zc_layer_norm_backward(dy, x, stats, w, dx, dw, db, workspace(5, cols)) == 0
+    s = values(stats)
+    wx, ww, wb, ux, uw, ub = model.norm_backward(values(dy), values(x), s[0], s[1], values(w))
+    assert (np.abs(values(dx) - wx) <= 72 * model.U * ux + model.half_step("f32", wx) * (1 + 2 ** -6)).all()
+    assert (np.abs(values(dw) - ww) <= 96 * model.U * uw).all()
+    assert (np.abs(values(db) - wb) <= 96 * model.U * ub).all()
