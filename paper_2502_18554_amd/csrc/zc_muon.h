@@ -32,11 +32,8 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) u32 LdsWord;
 
 constexpr int kMuonTensors = 64;                     // of one launch: their table travels in the kernel's arguments
-constexpr u32 kMuonAlong = 128;                      // rows of X, A, B and of X turned are filled up with zeros to a multiple of so many values
 constexpr float kMuonA = 3.4445f, kMuonB = -4.7750f, kMuonC = 2.0315f;
 constexpr float kMuonScale = 4096.0f;
-
-__host__ __device__ inline u64 muon_along(u64 n) { return (n + kMuonAlong - 1) / kMuonAlong * kMuonAlong; }
 
 struct MuonTensor {
   u8* at;                        // in the workspace
@@ -68,23 +65,6 @@ struct MuonArgs {
 };
 static_assert(sizeof(MuonArgs) <= 4096);
 // (The kernels read them where they lie: of a parameter that is used in many places, with an index, the compiler makes a copy in scratch memory.)
-
-// Places of a matrix's parts in its share of the workspace: X, X turned twice (one is read while the other is written), A, B; the low parts of two behind the high ones of each.
-struct MuonParts {
-  u64 row_x, row_t;                                  // values of a row of X; of X turned, A and B
-  u64 plane_x, plane_t, plane_a;                     // bytes
-  u64 x, t0, t1, a, b, bytes;
-  __host__ __device__ MuonParts(u32 r, u32 c, u32 planes) {
-    row_x = muon_along(c), row_t = muon_along(r);
-    plane_x = 2 * r * row_x, plane_t = 2 * c * row_t, plane_a = 2 * r * row_t;
-    x = 0;
-    t0 = x + planes * plane_x;
-    t1 = t0 + planes * plane_t;
-    a = t1 + planes * plane_t;
-    b = a + planes * plane_a;
-    bytes = b + planes * plane_a;
-  }
-};
 
 // The matrix that a tile or workgroup belongs to: a lane looks at one of them each, since a search one by one would wait for memory at each (24 matrices of 256 x 512: 4 us a launch).
 static_assert(kMuonTensors == 64);
@@ -248,20 +228,9 @@ __global__ __launch_bounds__(256) void muon_zeros_kernel(MuonArgs) {
 // other in LDS, their 16-byte blocks exchanged by the row's number, so that 16 lanes that read LDS together find 64 different banks.  An instruction multiplies eight values of 32 rows with as
 // many of 32 columns from lanes 0 .. 31, eight others from lanes 32 .. 63.  Which column of the tile a lane brings is free: it is chosen so that a lane ends with 16
 // neighbouring results of a row.  The requests run ahead into the workgroup's next tile too.
-enum { kMuonGram, kMuonPoly, kMuonUpdate, kMuonFinish };       // kMuonFinish + the weights' type
 
-// Rows of a tile as a buffer, seen from some bytes along them: rows behind the last one read as zeros.
-struct MuonRows {
-  u64 at;
-  u32 bytes;
-  __device__ void aim(const u8* base, u64 first, u64 rows, u64 stride, u32 most) {
-    at = reinterpret_cast<u64>(base) + first * stride;
-    bytes = u32(min(rows - first, u64(most)) * stride);
-  }
-  __device__ void move_on(u32 by) {
-    at += by;
-    bytes = bytes > by ? bytes - by : 0u;
-  }
+// Rows of a tile as a buffer: rows behind the last one read as zeros.
+struct MuonRows : MuonSpan {
   __device__ __amdgpu_buffer_rsrc_t buffer() const {
     return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(u64(uniform(u32(at))) | u64(uniform(u32(at >> 32))) << 32), 0, int(uniform(bytes)), 0x00027000);
   }
@@ -281,41 +250,14 @@ __device__ __forceinline__ void muon_hold(f32x16_t& sum) {
   else asm volatile("" : "+v"(sum));
 }
 
-// The tiles of a launch, and the operands of one.
+// The workgroup's tiles.
 template <int MODE>
-struct MuonTiles {
-  static constexpr bool kTriangle = MODE == kMuonGram || MODE == kMuonPoly;
-  u32 first, end, step;                              // the workgroup's own
-  __device__ explicit MuonTiles(u32 tiles) {         // every XCD has a run of neighbouring tiles (workgroups go round the eight XCDs)
-    const u32 xcd = blockIdx.x & 7u, share = tiles >> 3, more = tiles & 7u, begin = xcd * share + min(xcd, more);
-    first = begin + (blockIdx.x >> 3);
-    end = begin + share + (xcd < more ? 1u : 0u);
-    step = (gridDim.x + 7u - xcd) >> 3;
-  }
-  // Row and column of tile t of a matrix whose results are `down` x `across` tiles.
+struct MuonTiles : MuonShare {
+  __device__ explicit MuonTiles(u32 tiles) : MuonShare(tiles, blockIdx.x, gridDim.x) {}
   __device__ static void place(u32 t, u32 down, u32 across, u32& row, u32& col) {
-    if constexpr (kTriangle) {
-      // Strips of eight rows of tiles, down their columns: 32 s^2 + 4 s tiles are before strip s, which has 8 s whole columns and a triangle.
-      u32 s = u32(sqrtf(float(t) * (1.0f / 32.0f)));
-      while (s && 32 * s * s + 4 * s > t) --s;
-      while (32 * (s + 1) * (s + 1) + 4 * (s + 1) <= t) ++s;
-      u32 rest = t - (32 * s * s + 4 * s), c = 0;
-      const u32 high = min(8u, down - 8u * s);
-      if (rest < 8u * s * high) {
-        c = rest / high;
-        row = uniform(8u * s + rest - c * high);
-        col = uniform(c);
-      } else {
-        rest -= 8u * s * high;
-        while (rest >= high - c) rest -= high - c++;
-        row = uniform(8u * s + c + rest);
-        col = uniform(8u * s + c);
-      }
-    } else {
-      const u32 strip = t / (8u * across), rest = t - strip * 8u * across, high = min(8u, down - 8u * strip), c = rest / high;
-      col = uniform(c);
-      row = uniform(8u * strip + rest - c * high);
-    }
+    const MuonPlace p = muon_place<muon_symmetric(MODE)>(t, down, across, muon_symmetric(MODE) ? u32(sqrtf(float(t) * (1.0f / 32.0f))) : 0u);
+    row = uniform(p.row);
+    col = uniform(p.col);
   }
 };
 
@@ -525,7 +467,7 @@ __global__ __launch_bounds__(256, muon_groups(TM, TN, S)) void muon_product_kern
   const MuonArgs& a = kernel_args<MuonArgs, 0>();
   constexpr u32 KB = 64, RA = 64u * TM, RB = 64u * TN, BLOCKS = KB / 8, ROW = 2 * KB, AT_B = RA * ROW, STAGE = AT_B + RB * ROW;      // bytes of a row, of a stage
   constexpr u32 APART = 4096 / ROW, LOADS_A = AT_B / 4096, LOADS = STAGE / 4096, STEPS = KB / 16;    // rows between a thread's loads; its loads
-  constexpr bool TRIANGLE = MODE == kMuonGram || MODE == kMuonPoly, SMALL = TM * TN == 1;
+  constexpr bool TRIANGLE = muon_symmetric(MODE), SMALL = TM * TN == 1;
   static_assert(!TRIANGLE || TM == TN);
   __shared__ u32x4_t memory[S * STAGE / 16];
   const u32 tid = threadIdx.x, lane = tid & 63u, wave = uniform(tid >> 6), half = lane >> 5, in32 = lane & 31u;
@@ -548,13 +490,10 @@ __global__ __launch_bounds__(256, muon_groups(TM, TN, S)) void muon_product_kern
     u32 row, col;
     const u32 down = (r + RA - 1) / RA, across = TRIANGLE ? down : (c + RB - 1) / RB;
     MuonTiles<MODE>::place(asked.tile - of.first, down, across, row, col);
-    const u8* const at = of.at;
-    const u64 plane_a = MODE == kMuonGram ? parts.plane_x : parts.plane_a, plane_b = MODE == kMuonGram ? parts.plane_x : MODE == kMuonPoly ? parts.plane_a : parts.plane_t;
-    const u8* const from_a = at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : parts.b) + (asked.segment == 2 ? plane_a : 0);
-    const u8* const from_b = at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : a.which ? parts.t1 : parts.t0) + (asked.segment == 1 ? plane_b : 0);
-    const u64 along = MODE == kMuonGram ? parts.row_x : parts.row_t;
-    rows_a.aim(from_a, u64(row) * RA, r, 2 * along, RA);
-    rows_b.aim(from_b, u64(col) * RB, TRIANGLE ? r : c, 2 * along, RB);
+    const u64 at = reinterpret_cast<u64>(of.at);
+    const u64 along = muon_along_of(parts, MODE);
+    rows_a.aim(at + muon_operand_a(parts, MODE, asked.segment), u64(row) * RA, r, 2 * along, RA);
+    rows_b.aim(at + muon_operand_b(parts, MODE, a.which, asked.segment), u64(col) * RB, TRIANGLE ? r : c, 2 * along, RB);
     const u32 apart = uniform(u32(2 * along));
 #pragma unroll
     for (u32 k = 0; k < LOADS; ++k) {
@@ -623,7 +562,7 @@ __global__ __launch_bounds__(256, muon_groups(TM, TN, S)) void muon_product_kern
     const MuonOf of(a, tile);
     const u32 r = of.r, c = of.c;
     const MuonParts parts(r, c, a.planes);
-    const u32 stages = uniform(u32((MODE == kMuonGram ? parts.row_x : parts.row_t) / KB) * (a.planes > 1 ? 3u : 1u));
+    const u32 stages = uniform(u32(muon_along_of(parts, MODE) / KB) * (a.planes > 1 ? 3u : 1u));
     f32x16_t sum[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -706,14 +645,11 @@ __global__ __launch_bounds__(256, S == 2 ? 2 : 1) void muon_small_kernel(MuonArg
   const u32 r = of.r, c = of.c;
   const MuonParts parts(r, c, a.planes);
   u32 down, across;
-  constexpr bool TRIANGLE = MODE == kMuonGram || MODE == kMuonPoly;
+  constexpr bool TRIANGLE = muon_symmetric(MODE);
   const u32 tiles_down = (r + 31) / 32, tiles_across = TRIANGLE ? tiles_down : (c + 31) / 32;
   MuonTiles<MODE>::place(tiles.first - of.first, tiles_down, tiles_across, down, across);
-  const u64 along = MODE == kMuonGram ? parts.row_x : parts.row_t;
+  const u64 along = muon_along_of(parts, MODE), at = reinterpret_cast<u64>(of.at);
   const u32 per = u32(along / 64), stages = per * (a.planes > 1 ? 3u : 1u), apart = u32(2 * along);
-  const u64 plane_a = MODE == kMuonGram ? parts.plane_x : parts.plane_a, plane_b = MODE == kMuonGram ? parts.plane_x : MODE == kMuonPoly ? parts.plane_a : parts.plane_t;
-  const u8* const of_a = of.at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : parts.b);
-  const u8* const of_b = of.at + (MODE == kMuonGram ? parts.x : MODE == kMuonPoly ? parts.a : a.which ? parts.t1 : parts.t0);
   const auto key_a = [](u32 row) { return row >> 1 & 7u; };
   const auto key_b = [](u32 row) { return (row >> 1 & 1u) | (row >> 3 & 2u) | (row & 4u); };
   u32 mine_a[4], mine_b[4];
@@ -724,21 +660,20 @@ __global__ __launch_bounds__(256, S == 2 ? 2 : 1) void muon_small_kernel(MuonArg
     mine_b[k] = row * apart + 16u * ((lane ^ key_b(row)) & 7u);
   }
   const u32 lds0 = u32(reinterpret_cast<uintptr_t>((LdsWord*)&memory[0])) + wave * S * STAGE;
-  u32 ask_segment = 0, ask_at = wave, asked = wave;  // the stage that is asked for next, in its product of parts and in all
+  MuonQuarter asked{0, wave, wave};
   const auto ask = [&](u32 place) {
-    while (ask_at >= per) ask_at -= per, ++ask_segment;
+    asked.settle(per);
     MuonRows rows_a, rows_b;
-    rows_a.aim(of_a + (ask_segment == 2 ? plane_a : 0), u64(down) * 32, r, apart, 32);
-    rows_b.aim(of_b + (ask_segment == 1 ? plane_b : 0), u64(across) * 32, TRIANGLE ? r : c, apart, 32);
-    rows_a.move_on(128 * ask_at);
-    rows_b.move_on(128 * ask_at);
-    if (asked >= stages) rows_a.bytes = rows_b.bytes = 0;      // (behind the last stage there is nothing to ask for)
+    rows_a.aim(at + muon_operand_a(parts, MODE, asked.segment), u64(down) * 32, r, apart, 32);
+    rows_b.aim(at + muon_operand_b(parts, MODE, a.which, asked.segment), u64(across) * 32, TRIANGLE ? r : c, apart, 32);
+    rows_a.move_on(128 * asked.at);
+    rows_b.move_on(128 * asked.at);
+    if (asked.all >= stages) rows_a.bytes = rows_b.bytes = 0;      // (behind the last stage there is nothing to ask for)
 #pragma unroll
     for (u32 k = 0; k < 4; ++k) muon_load_to_lds(rows_a.buffer(), lds0 + place + 1024u * k, mine_a[k]);
 #pragma unroll
     for (u32 k = 0; k < 4; ++k) muon_load_to_lds(rows_b.buffer(), lds0 + place + 4096u + 1024u * k, mine_b[k]);
-    ask_at += 4;
-    asked += 4;
+    asked.next();
   };
   const u32 lane_b = (in32 & 3u) + 16u * ((in32 >> 2) & 1u) + 4u * (in32 >> 3);
   typedef const __attribute__((address_space(3))) u32x4_t LdsBlock;

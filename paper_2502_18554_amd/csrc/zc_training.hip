@@ -142,7 +142,7 @@ bool share_results(int k, const size_t* rows, const size_t* cols, void* const* p
 
 u64 muon_tiles(const MuonTensor& t, int mode, u64 high, u64 wide) {
   const u64 down = (t.r + high - 1) / high, across = (t.c + wide - 1) / wide;
-  return mode == kMuonGram || mode == kMuonPoly ? down * (down + 1) / 2 : down * across;
+  return muon_symmetric(mode) ? down * (down + 1) / 2 : down * across;
 }
 template <int MODE>
 void count_muon_tiles(MuonArgs& a, u64 high, u64 wide) {
