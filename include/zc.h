@@ -418,7 +418,7 @@ int zc_embedding_backward(const void* d_dy, int dy_type, size_t dy_stride, const
  * param_type, grad_type, d_copies, copy_type, d_grad_scale: as in zc_adamw (a scale that is not finite: nothing changes).  A gradient with a value that is not finite makes its
  * matrix's p' and what it touches of m' NaNs.  No two results are the same memory.  d_state: zc_muon_state_bytes bytes, 16-byte aligned, zeros before the first step: m of all matrices in their order as binary32 values, each
  * filled up to a multiple of 32 of them.  d_ws: zc_muon_workspace_bytes bytes, 256-byte aligned, its content irrelevant, one for calls that may overlap.  Equal calls
- * give equal results.  Up to 2^20 rows and columns, 1 to 100 iterations.  Errors: ARG, HIP. */
+ * give equal results.  Up to 2^20 rows and columns, 1 to 100 iterations.  Errors: ARG (also lr factor or 1 - lr weight_decay not finite, or momentum 1, in binary32), HIP. */
 #define ZC_MUON_NESTEROV 1u
 #define ZC_MUON_MATCH_RMS 2u
 #define ZC_MUON_WIDE 4u

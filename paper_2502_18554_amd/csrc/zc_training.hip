@@ -124,6 +124,11 @@ u64 muon_workspace(int k, const size_t* rows, const size_t* cols, u32 planes) {
   return most;
 }
 
+// What lr is multiplied by for a matrix.
+double muon_factor(u64 r, u64 c, unsigned flags) {
+  return flags & ZC_MUON_MATCH_RMS ? 0.2 * std::sqrt(double(larger(r, c))) : r > c ? std::sqrt(double(r) / double(c)) : 1.0;
+}
+
 // Whether two of a call's results begin at one place: launches take many matrices together, so that one would be lost.
 bool share_results(int k, const size_t* rows, const size_t* cols, void* const* params, void* const* copies) {
   for (int i = 0; i < k; ++i) {
@@ -354,6 +359,7 @@ int zc_muon(int k, const size_t* rows, const size_t* cols, void* const* d_params
             size_t ws_bytes, void* hip_stream) {
   if (!muon_sizes_valid(k, rows, cols) || (k > 0 && (!d_params || !d_grads)) || !type_valid(param_type) || !type_valid(grad_type) || (d_copies && !type_valid(copy_type))) return ZC_ERR_ARG;
   if (!(std::isfinite(lr) && lr >= 0 && momentum >= 0 && momentum < 1 && std::isfinite(weight_decay) && weight_decay >= 0) || iterations < 1 || iterations > kMostIterations) return ZC_ERR_ARG;
+  if (!(float(momentum) < 1) || !std::isfinite(float(1 - lr * weight_decay))) return ZC_ERR_ARG;
   if ((flags & ~(ZC_MUON_NESTEROV | ZC_MUON_MATCH_RMS | ZC_MUON_WIDE)) || !aligned(d_grad_scale, 4) || !aligned(d_state, 16) || !aligned(d_ws, 256)) return ZC_ERR_ARG;
   const u32 planes = flags & ZC_MUON_WIDE ? 2 : 1;
   const u64 state = zc_muon_state_bytes(k, rows, cols), ws = muon_workspace(k, rows, cols, planes);
@@ -362,6 +368,7 @@ int zc_muon(int k, const size_t* rows, const size_t* cols, void* const* d_params
     if (rows[i] == 0 || cols[i] == 0) continue;
     if (!d_params[i] || !d_grads[i] || !aligned(d_params[i], value_bytes(param_type)) || !aligned(d_grads[i], value_bytes(grad_type))) return ZC_ERR_ARG;
     if (d_copies && !aligned(d_copies[i], value_bytes(copy_type))) return ZC_ERR_ARG;
+    if (!std::isfinite(float(lr * muon_factor(rows[i], cols[i], flags)))) return ZC_ERR_ARG;
   }
   if (share_results(k, rows, cols, d_params, d_copies)) return ZC_ERR_ARG;
   const auto stream = static_cast<hipStream_t>(hip_stream);
@@ -386,8 +393,7 @@ int zc_muon(int k, const size_t* rows, const size_t* cols, void* const* d_params
         t.grad = d_grads[i];
         t.m = m;
         t.r = smaller(r, c), t.c = larger(r, c);
-        const double factor = flags & ZC_MUON_MATCH_RMS ? 0.2 * std::sqrt(double(t.c)) : r > c ? std::sqrt(double(r) / double(c)) : 1.0;
-        t.step = float(lr * factor);
+        t.step = float(lr * muon_factor(r, c, flags));
         t.turned = r > c;
         ++a.tensors;
       }
