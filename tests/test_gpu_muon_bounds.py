@@ -75,3 +75,41 @@ def test_thin_matrices_in_two_parts(rows, cols):
     assert torch.equal(m, grad)
     (_, q, r), _ = step([gradient(30, 50, g), grad, grad], True)
     assert off(values(q), want) <= room and torch.equal(q, r)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf"), 3e38])
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("wide", [False, True])
+def test_gradients_that_are_not_finite(bad, nesterov, wide):
+    """(3e38 times the scale of two is infinite.)  The matrix's weights become NaNs, the momentum only where the gradient is not finite; other matrices stay what they are without it."""
+    g = generator(12)
+    shapes = [(40, 50), (150, 20), (1, 1), (40, 50)]
+    grads = [gradient(*s, g) for s in shapes]
+    scale = torch.full((1,), 2.0, device=DEV)
+    clean, p = ([torch.ones(s, device=DEV) for s in shapes] for _ in range(2))
+    states = [state_of(shapes) for _ in range(2)]
+    how = dict(nesterov=nesterov, wide=wide, d_grad_scale=scale)
+    assert zc.zc_muon(clean, grads, states[0], workspace(shapes, wide), 0.1, **how) == 0
+    grads[1][149, 3] = grads[2][0, 0] = bad
+    assert zc.zc_muon(p, grads, states[1], workspace(shapes, wide), 0.1, **how) == 0
+    assert torch.equal(p[0], clean[0]) and torch.equal(p[3], clean[3])
+    assert bool(p[1].isnan().all()) and bool(p[2].isnan().all())
+    for i, (got, want) in enumerate(zip(parts_of(states[1], shapes), parts_of(states[0], shapes))):
+        touched = torch.zeros(shapes[i], dtype=torch.bool, device=DEV)
+        if i in (1, 2):
+            touched[-1, 3 if i == 1 else 0] = True
+        assert not bool(got[touched].isfinite().any()) and torch.equal(got[~touched], want[~touched])
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_gradients_under_the_floor(wide):
+    """Norms under 1e-7, by which X is divided then.  6e-9: X is as any other.  6e-30: X, 6e-23 at 2^12, is less than half of binary16's smallest number, 3e-8, and so nothing."""
+    g = generator(13)
+    grad = torch.rand(50, 60, generator=g, device=DEV).sub_(0.5).mul_(4e-10)
+    (p,), _ = step([grad], wide)
+    exact = model.orthogonalised(values(grad), 5, 0)
+    rounded = model.orthogonalised(values(grad), 5, 2 if wide else 1)
+    assert 0.01 < np.abs(exact).max() < 1
+    assert off(values(p), -exact) <= 1.5 * off(rounded, exact) + 2.0 ** -18
+    (p,), _ = step([grad * 1e-21], wide)
+    assert not bool(p.any())
