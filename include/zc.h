@@ -416,7 +416,7 @@ int zc_embedding_backward(const void* d_dy, int dy_type, size_t dy_stride, const
  * The products' operands are X, A and B rounded to 11 bits (binary16, scaled by 2^12), with ZC_MUON_WIDE to 22 bits (two of them; three times the work), sums are in
  * binary32: p' is off by some 2^-9, with ZC_MUON_WIDE 2^-18 (up to 2^-16 where a side has more than 4096 values), of lr factor times a typical value of X.
  * param_type, grad_type, d_copies, copy_type, d_grad_scale: as in zc_adamw (a scale that is not finite: nothing changes).  A gradient with a value that is not finite, or whose
- * product with the scale is not, makes its matrix's p' NaNs and what it touches of m' infinite or NaN.  No two results are the same memory.  d_state: zc_muon_state_bytes bytes, 16-byte aligned, zeros before the first step: m of all matrices in their order as binary32 values, each
+ * product with the scale is not, makes its matrix's p' NaNs and what it touches of m' infinite or NaN.  No two results, d_state among them, overlap.  d_state: zc_muon_state_bytes bytes, 16-byte aligned, zeros before the first step: m of all matrices in their order as binary32 values, each
  * filled up to a multiple of 32 of them.  d_ws: zc_muon_workspace_bytes bytes, 256-byte aligned, its content irrelevant, one for calls that may overlap.  Equal calls
  * give equal results.  Up to 2^20 rows and columns, 1 to 100 iterations.  Errors: ARG (also lr factor or 1 - lr weight_decay not finite, or momentum 1, in binary32), HIP. */
 #define ZC_MUON_NESTEROV 1u

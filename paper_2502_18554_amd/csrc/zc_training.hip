@@ -1,7 +1,10 @@
 // C ABI of the other calls of a training step: layer norm, embedding, and the optimiser's step for matrices.  Argument checks and launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
+#include <memory>
+#include <new>
 
 #include "zc_embedding.h"
 #include "zc_muon.h"
@@ -129,20 +132,26 @@ double muon_factor(u64 r, u64 c, unsigned flags) {
   return flags & ZC_MUON_MATCH_RMS ? 0.2 * std::sqrt(double(larger(r, c))) : r > c ? std::sqrt(double(r) / double(c)) : 1.0;
 }
 
-// Whether two of a call's results begin at one place: launches take many matrices together, so that one would be lost.
-bool share_results(int k, const size_t* rows, const size_t* cols, void* const* params, void* const* copies) {
+// Whether no two of a call's results, the momentum among them, have a byte in common: launches take many matrices together, so that one would be lost.  Not known (no memory to sort them in): -1.
+struct MuonResult {
+  uintptr_t begin, end;
+};
+int results_apart(int k, const size_t* rows, const size_t* cols, void* const* params, int param_type, void* const* copies, int copy_type, const void* state, u64 state_bytes) {
+  const std::unique_ptr<MuonResult[]> all(new (std::nothrow) MuonResult[2 * size_t(k) + 1]);
+  if (!all) return -1;
+  size_t n = 0;
+  const auto add = [&](const void* p, u64 bytes) {
+    if (p && bytes) all[n++] = {reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes};
+  };
+  add(state, state_bytes);
   for (int i = 0; i < k; ++i) {
-    if (rows[i] == 0 || cols[i] == 0) continue;
-    const void *const p = params[i], *const c = copies ? copies[i] : nullptr;
-    bool twice = p == c;
-    for (int j = 0; j < i; ++j) {
-      const bool there = rows[j] != 0 && cols[j] != 0;
-      const void *const of = params[j], *const copy = copies ? copies[j] : nullptr;
-      twice |= there && (of == p || of == c || (copy && (copy == p || copy == c)));
-    }
-    if (twice) return true;
+    add(params[i], u64(rows[i]) * cols[i] * value_bytes(param_type));
+    if (copies) add(copies[i], u64(rows[i]) * cols[i] * value_bytes(copy_type));
   }
-  return false;
+  std::sort(all.get(), all.get() + n, [](const MuonResult& a, const MuonResult& b) { return a.begin < b.begin; });
+  for (size_t i = 1; i < n; ++i)
+    if (all[i].begin < all[i - 1].end) return 0;
+  return 1;
 }
 
 u64 muon_tiles(const MuonTensor& t, int mode, u64 high, u64 wide) {
@@ -370,7 +379,8 @@ int zc_muon(int k, const size_t* rows, const size_t* cols, void* const* d_params
     if (d_copies && !aligned(d_copies[i], value_bytes(copy_type))) return ZC_ERR_ARG;
     if (!std::isfinite(float(lr * muon_factor(rows[i], cols[i], flags)))) return ZC_ERR_ARG;
   }
-  if (share_results(k, rows, cols, d_params, d_copies)) return ZC_ERR_ARG;
+  const int apart = results_apart(k, rows, cols, d_params, param_type, d_copies, copy_type, d_state, state);
+  if (apart != 1) return apart ? ZC_ERR_HIP : ZC_ERR_ARG;
   const auto stream = static_cast<hipStream_t>(hip_stream);
   float* m = static_cast<float*>(d_state);
   for (int i = 0; i < k;) {
