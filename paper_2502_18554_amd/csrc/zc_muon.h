@@ -24,6 +24,7 @@
 
 #include "zc_muon_ask.h"
 #include "zc_rows.h"
+#include "zc_to_lds.h"
 
 namespace zc {
 
@@ -236,13 +237,6 @@ struct MuonRows : MuonSpan {
   }
 };
 
-// 16 bytes a lane to LDS, at `to` and on.  (Written out: of its own loads to LDS the compiler thinks that any read of LDS may have to wait for them.  m0 is reserved, so
-// that it cannot be named among what is overwritten: nothing else in these kernels may use it.)
-// The buffer's words may come from a vector instruction (uniform values that the compiler has in lanes) right before: a load reads them five wait states later at the earliest, which the compiler
-// keeps for its own loads, but not for what is written out.  With fewer the load would see the words of before, another place or length.
-__device__ inline void muon_load_to_lds(__amdgpu_buffer_rsrc_t from, u32 to, u32 lane_offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(lane_offset), "s"(from) : "memory");
-}
 // Keeps an instruction's sums at their place, in the matrix instructions' own registers where a wave is alone on its SIMD (the compiler has them there then).
 template <bool OWN>
 __device__ __forceinline__ void muon_hold(f32x16_t& sum) {
@@ -514,8 +508,8 @@ __global__ __launch_bounds__(256, muon_groups(TM, TN, S)) void muon_product_kern
   const u32 lds0 = u32(reinterpret_cast<uintptr_t>((LdsWord*)&memory[0]));
   const auto ask = [&](u32 place, u32 i) {           // place: of the stage in LDS, in bytes
     const u32 to = lds0 + wave * 1024u + place + 4096u * i;
-    if (i < LOADS_A) muon_load_to_lds(rows_a.buffer(), to, mine_a[i]);
-    else muon_load_to_lds(rows_b.buffer(), to, mine_b[i - LOADS_A]);
+    if (i < LOADS_A) load_to_lds(rows_a.buffer(), to, mine_a[i]);
+    else load_to_lds(rows_b.buffer(), to, mine_b[i - LOADS_A]);
   };
 
   const u32 wave_a = (wave >> 1) * 32u * TM, wave_b = (wave & 1u) * 32u * TN;
@@ -670,9 +664,9 @@ __global__ __launch_bounds__(256, S == 2 ? 2 : 1) void muon_small_kernel(MuonArg
     rows_b.move_on(128 * asked.at);
     if (asked.all >= stages) rows_a.bytes = rows_b.bytes = 0;      // (behind the last stage there is nothing to ask for)
 #pragma unroll
-    for (u32 k = 0; k < 4; ++k) muon_load_to_lds(rows_a.buffer(), lds0 + place + 1024u * k, mine_a[k]);
+    for (u32 k = 0; k < 4; ++k) load_to_lds(rows_a.buffer(), lds0 + place + 1024u * k, mine_a[k]);
 #pragma unroll
-    for (u32 k = 0; k < 4; ++k) muon_load_to_lds(rows_b.buffer(), lds0 + place + 4096u + 1024u * k, mine_b[k]);
+    for (u32 k = 0; k < 4; ++k) load_to_lds(rows_b.buffer(), lds0 + place + 4096u + 1024u * k, mine_b[k]);
     asked.next();
   };
   const u32 lane_b = (in32 & 3u) + 16u * ((in32 >> 2) & 1u) + 4u * (in32 >> 3);

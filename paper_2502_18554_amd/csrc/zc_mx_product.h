@@ -5,6 +5,7 @@
 #pragma once
 
 #include "zc_mx.h"
+#include "zc_to_lds.h"
 
 namespace zc {
 
@@ -110,14 +111,6 @@ struct MxRows {
   }
 };
 constexpr u64 kMostTileStride = u64(1) << 23;       // (256 rows are less than 2^32 bytes)
-
-// 16 bytes a lane to LDS, at `to` and on.  (Written out: of its own loads to LDS the compiler thinks that any read of LDS may have to wait for them.  m0 is reserved, so
-// that it cannot be named among what is overwritten: nothing else in these kernels may use it, as another load to LDS, a message or an indexed register would.)
-// The buffer's words may come from a vector instruction (uniform values that the compiler has in lanes) right before: a load reads them five wait states later at the earliest, which the compiler
-// keeps for its own loads, but not for what is written out.  With fewer the load would see the words of before, another place or length.
-__device__ inline void mx_load_to_lds(__amdgpu_buffer_rsrc_t from, u32 to, u32 lane_offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(lane_offset), "s"(from) : "memory");
-}
 
 template <typename T>
 __device__ inline const __attribute__((address_space(3))) T* mx_lds(u32 at) {
@@ -297,8 +290,8 @@ __global__ __launch_bounds__(256, TM * TN > 4 ? 1 : TM * TN > 1 ? 2 : 4) void mx
   const u32 lds0 = u32(reinterpret_cast<uintptr_t>((MxLdsWord*)&memory[0]));
   const auto ask = [&](u32 u, u32 i) {
     const u32 to = lds0 + wave * 1024u;
-    if (i < RA / 32) mx_load_to_lds(rows_a.buffer(), to + u * (RA * 128u) + 4096u * i, from_a[i]);
-    else mx_load_to_lds(rows_b.buffer(), to + AT_B + u * (RB * 128u) + 4096u * (i - RA / 32), from_b[i - RA / 32]);
+    if (i < RA / 32) load_to_lds(rows_a.buffer(), to + u * (RA * 128u) + 4096u * i, from_a[i]);
+    else load_to_lds(rows_b.buffer(), to + AT_B + u * (RB * 128u) + 4096u * (i - RA / 32), from_b[i - RA / 32]);
   };
   const auto next_stage = [&] {
     rows_a.move_on(128);
