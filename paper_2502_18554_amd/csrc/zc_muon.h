@@ -628,9 +628,10 @@ __global__ __launch_bounds__(256, muon_groups(TM, TN, S)) void muon_product_kern
 // ---- Few and small results: workgroups make tiles of 32 x 32, and their four waves take every fourth stage of 64 values each, by themselves: a wave's requests go to a part of LDS of its own, and
 // it waits for nobody.  At the end the first wave adds the four sums.  (Tiles of 64 of the sizes for which this is there are bound by what a workgroup waits for itself: three matrices of
 // 333 x 1531 in two parts, 63 tiles on 256 CUs, 21 us for X X^T, 0.25 us a stage.)
-template <int S, int MODE>
-__global__ __launch_bounds__(256, S == 2 ? 2 : 1) void muon_small_kernel(MuonArgs) {
+template <int MODE>
+__global__ __launch_bounds__(256, 2) void muon_small_kernel(MuonArgs) {
   const MuonArgs& a = kernel_args<MuonArgs, 0>();
+  constexpr int S = 2;                               // stages of a wave in LDS
   constexpr u32 STAGE = 8192;                        // of a wave: 32 rows of each operand
   __shared__ u32x4_t memory[4 * S * STAGE / 16];
   const u32 lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), half = lane >> 5, in32 = lane & 31u;

@@ -209,7 +209,7 @@ void launch_muon_product(MuonArgs& a, hipStream_t stream) {
     if (cost[t] < cost[best]) best = t;
   if (best == 0) {
     count_muon_tiles<MODE>(a, 32, 32);
-    hipLaunchKernelGGL((muon_small_kernel<2, MODE>), dim3(a.count), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((muon_small_kernel<MODE>), dim3(a.count), dim3(256), 0, stream, a);
   } else if (best == 1) {
     launch_muon_tiles<1, 1, 4, MODE>(a, stream);
   } else if (best == 2) {
