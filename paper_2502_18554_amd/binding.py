@@ -727,7 +727,7 @@ def zc_muon_workspace_bytes(shapes, wide=False):
 def zc_muon(d_params, d_grads, d_state, d_ws, lr, momentum=0.95, weight_decay=0.0, iterations=5, nesterov=True, match_rms=False, wide=False, d_copies=None, d_grad_scale=None,
             stream=None):
     """One step with orthogonalised momentum over the matrices of the list d_params (contiguous, of one type; d_grads: as many of the same shapes, of one type), in
-    place.  d_copies: None, or a list with a matrix or None for each.  Returns the status."""
+    place.  d_copies: None, or a list with a matrix or None for each; one that is the matrix of d_params itself, as .to() of its own type gives, is left out.  Returns the status."""
     lib()
     flags = (ZC_MUON_NESTEROV if nesterov else 0) | (ZC_MUON_MATCH_RMS if match_rms else 0) | (ZC_MUON_WIDE if wide else 0)
     if _native_layers:
@@ -745,7 +745,7 @@ def zc_muon(d_params, d_grads, d_state, d_ws, lr, momentum=0.95, weight_decay=0.
         return ZC_ERR_ARG
     _, rows, cols = _shapes(shapes)
     lists = [_words([t.data_ptr() for t in d_params]), _words([t.data_ptr() for t in d_grads]),
-             _words([t.data_ptr() if t is not None else 0 for t in d_copies]) if d_copies is not None else (None, None)]
+             _words([0 if t is None or (t.dtype == p.dtype and t.data_ptr() == p.data_ptr()) else t.data_ptr() for t, p in zip(d_copies, d_params)]) if d_copies is not None else (None, None)]
     if not 0 <= int(iterations) < 1 << 31:
         return ZC_ERR_ARG
     return lib().zc_muon(k, rows[1], cols[1], lists[0][1], _one_type(d_params), lists[1][1], _one_type(d_grads), lists[2][1], _one_type(copies), _p(d_state),

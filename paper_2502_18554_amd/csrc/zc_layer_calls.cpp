@@ -390,6 +390,9 @@ PyObject* muon(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       (copies && !matrices_of(a[9], k, true, device, sizes, at.data() + 2 * k, types[2])) || !workspace_of(a[2], state, state_bytes) || !workspace_of(a[3], ws, ws_bytes) ||
       !bias_of(a[10], 1, scale) || !stream_of(a[11], stream))
     return not_this_way();
+  if (copies && types[2] == types[0])
+    for (size_t i = 0; i < size_t(k); ++i)                 // (a matrix is its own copy of its own type)
+      if (at[size_t(2 * k) + i] == at[i]) at[size_t(2 * k) + i] = nullptr;
   int st;
   Py_BEGIN_ALLOW_THREADS
   st = g_calls.muon(int(k), sizes.data(), sizes.data() + k, at.data(), types[0], const_cast<const void* const*>(at.data() + k), types[1], copies ? at.data() + 2 * k : nullptr, types[2], state,

@@ -195,7 +195,7 @@ void launch_muon_product(MuonArgs& a, hipStream_t stream) {
   }
   const auto stages = [&](int t) { return along[t] / tiles[t]; };
   const auto turns = [&](int t, double at_once) { return std::ceil(tiles[t] / at_once); };
-  const double cost[kMuonKindsOf] = {2 + turns(0, 512) * (2.3 + (tiles[0] <= 512 ? 0.075 : 0.16) * stages(0)),
+  const double cost[kMuonKindsOf] = {2 + turns(0, 512) * (2.3 + (tiles[0] <= 256 ? 0.075 : 0.16) * stages(0)),
                                      3 + (tiles[1] <= 256 ? 2 + 0.25 * stages(1) : turns(1, 512) * (3 + 0.5 * stages(1))),
                                      tiles[2] <= 256 ? 8 + 0.46 * stages(2) : 4 + turns(2, 512) * (12 + 1.1 * stages(2)),
                                      turns(3, 256) * (12 + (tiles[3] <= 160 ? 0.68 : 0.83) * stages(3)),

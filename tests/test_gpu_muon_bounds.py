@@ -13,7 +13,7 @@ import torch
 
 import paper_2502_18554_amd as zc
 import training_model as model
-from test_gpu_muon import DEV, generator, gradient, off, parts_of, state_of, values, workspace
+from test_gpu_muon import DEV, TYPES, generator, gradient, off, parts_of, state_of, values, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -113,3 +113,29 @@ def test_gradients_under_the_floor(wide):
     assert off(values(p), -exact) <= 1.5 * off(rounded, exact) + 2.0 ** -18
     (p,), _ = step([grad * 1e-21], wide)
     assert not bool(p.any())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_copies_that_are_the_matrices_themselves(kind, monkeypatch):
+    """What .to() gives for the type that a tensor has already: the same call without them.  A copy that is another matrix is refused."""
+    g = generator(14)
+    shapes = [(70, 40), (64, 64), (5, 90)]
+    grads = [gradient(*s, g) for s in shapes]
+    start = [torch.randn(s, generator=g, device=DEV).to(TYPES[kind]) for s in shapes]
+
+    def run(copies):
+        p = [t.clone() for t in start]
+        others = [torch.zeros_like(t) for t in p]
+        state = state_of(shapes)
+        assert zc.zc_muon(p, grads, state, workspace(shapes, False), 0.1, d_copies=copies(p, others)) == 0
+        return (*p, state), others
+
+    for _ in range(2):
+        want, _ = run(lambda p, o: None)
+        for copies in (lambda p, o: [t.to(TYPES[kind]) for t in p], lambda p, o: [p[0], o[1], p[2]]):
+            got, others = run(copies)
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert torch.equal(others[1], want[1]) and not bool(others[0].any())
+        p = [t.clone() for t in start]
+        assert zc.zc_muon([p[0], p[0].clone()], [grads[0]] * 2, state_of(shapes[:1] * 2), workspace(shapes[:1] * 2, False), 0.1, d_copies=[torch.zeros_like(p[0]), p[0]]) == zc.binding.ZC_ERR_ARG
+        monkeypatch.setattr(zc.binding, "_native_layers", None)
