@@ -15,9 +15,10 @@
 // A and B are symmetric: the tiles on and under the diagonal are computed and written twice.  X is kept as it is and turned, since the instructions take both operands along
 // the sum: X X^T sums along the columns, B X along the rows.  All matrices of a list go through each product in one launch.
 //
-// Bound by the matrix instructions where the matrices are large: 4096 x 8192 takes 139, 82 and 248 us for the three products (138 GFLOP of the symmetric half, 69, 275: 1.0, 0.84 and 1.11 PFLOP/s,
-// where a library's product of 8192^3 reaches 1.4), at 1.7 to 1.8 GHz.  What is between: the results' way to memory after the last instruction, as they are and turned, some 25 us a product,
-// and tiles that do not fill the last turn of CUs.  24 matrices of 256 x 512 take 6, 6 and 10 us: a launch and the latencies of one tile.
+// Bound by the matrix instructions where the matrices are large: 4096 x 8192 takes 146, 84 and 247 us for the three products (138 GFLOP of the symmetric half, 69, 275: 0.94, 0.82 and 1.11 PFLOP/s,
+// where a library's product of 8192^3 reaches 1.4), at 1.7 to 2.1 GHz.  What is between: the results' way to memory after the last instruction, as they are and turned, some 25 us a product,
+// and tiles that do not fill the last turn of CUs.  24 matrices of 256 x 512 take 7, 6.5 and 11 us: a launch and the latencies of one tile
+// (waves wait for 65, 65 and 46 % of their time, matrix instructions are busy for 3, 1 and 4 %).
 #pragma once
 
 #include <utility>
@@ -627,7 +628,7 @@ __global__ __launch_bounds__(256, muon_groups(TM, TN, S)) void muon_product_kern
 
 // ---- Few and small results: workgroups make tiles of 32 x 32, and their four waves take every fourth stage of 64 values each, by themselves: a wave's requests go to a part of LDS of its own, and
 // it waits for nobody.  At the end the first wave adds the four sums.  (Tiles of 64 of the sizes for which this is there are bound by what a workgroup waits for itself: three matrices of
-// 333 x 1531 in two parts, 63 tiles on 256 CUs, 21 us for X X^T, 0.25 us a stage.)
+// 333 x 1531 in two parts, 63 tiles on 256 CUs, 24 us for X X^T, 0.3 us a stage; here 10.4.)
 template <int MODE>
 __global__ __launch_bounds__(256, 2) void muon_small_kernel(MuonArgs) {
   const MuonArgs& a = kernel_args<MuonArgs, 0>();

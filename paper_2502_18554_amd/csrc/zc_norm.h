@@ -11,8 +11,9 @@
 // the columns, which a workgroup writes once.  A second launch adds the workgroups' sums in their order, so that equal calls give equal results.
 //
 // How many lanes share a row grows with its length, so that a lane has 8 to 32 values: 16 up to 128 values, a wave up to 2048, 256 up to 8192, 512 up to 16384.  Measured: 16384 rows of 4096 values,
-// 32 bits to 16 with statistics, 79 us (5.1 TB/s, a copy's rate); their gradients, dx added to 32 bits, 175 us (5.4 TB/s) and 5 us for the workgroups' sums.  512 rows of 16384 values of 16 bits
-// 11.5, 18 and 6.4 us: a row for each of 256 workgroups and one more, so that little is on its way at once; a row of 4096 values 3.2 us, 333 of 1001 4.6, 6 and 3.9: latency.
+// 32 bits to 16 with statistics, 80 us (5.0 TB/s, a copy's rate); their gradients, dx added to 32 bits, 169 us (5.6 TB/s) and 5 us for the workgroups' sums.  512 rows of 16384 values of 16 bits
+// 11.6, 18 and 6.5 us: a row for each of 256 workgroups and one more, so that little is on its way at once; a row of 4096 values 3.2 us, 333 of 1001 4.7, 6 and 3.8: latency.
+// Longer rows are read three times: 4096 of 32768 values of 16 bits 173 us (3.1 TB/s of what has to be read and written; 16384 values in registers 44, 6.1), their gradients 306.
 #pragma once
 
 #include "zc_rows.h"

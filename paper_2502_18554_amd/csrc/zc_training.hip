@@ -173,10 +173,14 @@ void launch_muon_tiles(MuonArgs& a, hipStream_t stream) {
   const u32 at_once = 256 * muon_groups(TM, TN, S);
   hipLaunchKernelGGL((muon_product_kernel<TM, TN, S, MODE>), dim3(a.count < at_once ? a.count : at_once), dim3(256), 0, stream, a);
 }
-// The kind of tile that takes the least time, in us, by what a turn of all CUs has been measured to take: a tile's begin and end, and its stages of 64 values.
-// (X X^T of three matrices of 333 x 1531 in two parts: tiles of 32, 64 and 128 9.5, 21 and 33 us, and the third product by 64, 64 x 128 and 128 17.7, 13.6 and 18.3; X X^T of 24 of 256 x 512 8.4,
-// 6.9 and 9.1.  Six of 1024 x 4096 in two parts, X X^T by tiles of 64, 128, 192 and 256 146, 95, 141 and 223, the third product by 128, 128 x 256, 192 and 256 209, 175, 208 and 184;
-// 4096 x 8192: X X^T by 128, 192 and 256 181, 123 and 154, the third product 252, 247 and 215.)
+// The kind of tile that takes the least time, in us, by what a turn of all CUs takes: a tile's begin and end, and its stages of 64 values.  The constants were measured on single products, over and over on
+// the same operands; in steps they are low by some tenth, all alike.  What the kinds take in steps, us, the one that the rule picks with a *:
+//   3 of 333 x 1531, two parts    X X^T by 32*, 64, 128, 192  10.4, 24.4, 38.8, 63.8    A A by the same  6.1*, 12.1, 19.7, 33.4    B X by 32, 64, 64 x 128*, 128, 192  21.7, 16.6, 17.2, 20.8, 32.6
+//   24 of 256 x 512               X X^T by 32, 64*, 128  8.2, 6.9, 10.2    A A  7.6, 6.0*, 9.0    B X by 32, 64, 64 x 128*, 128, 128 x 256  18.8, 10.4, 10.5, 10.3, 14.1
+//   6 of 1024 x 4096, two parts   X X^T by 64, 128*, 192, 256  163, 114, 161, 252    A A  53, 40*, 62    B X by 64 x 128, 128, 128 x 256*, 192, 256  261, 220, 193, 236, 210
+//   4096 x 8192                   X X^T by 128, 192*, 256  201, 147, 184    A A by 64, 128, 192*  149, 111, 86    B X by 128, 128 x 256, 192, 256*  298, 284, 291, 255
+// A stage takes longer the more CUs work: X X^T of matrices of 384 x 8192 (128 stages) by 192 takes 96, 111, 125, 131 and 132 us with 18, 60, 120, 159 and 192 tiles, of 512 x 8192 by 256 152, 181, 195,
+// 202 and 214; the rule has one step of it, at 160.  By 32 it is whether a CU has one workgroup or two (320 x 4096, 64 stages: 9.3, 9.4, 15.0, 20.0 and 26.8 us with 110, 220, 495, 550 and 990 tiles).
 struct MuonKind {
   u64 high, wide;
 };
@@ -213,8 +217,8 @@ void launch_muon_product(MuonArgs& a, hipStream_t stream) {
   } else if (best == 1) {
     launch_muon_tiles<1, 1, 4, MODE>(a, stream);
   } else if (best == 2) {
-    // Where every CU has one tile at most, a third stage lies in LDS instead of a second workgroup's (X X^T of six matrices of 1024 x 4096 in two parts, 216 tiles, 95 us, 126 by two;
-    // of 4096 x 8192, 528 tiles, 181 by two).
+    // Where every CU has one tile at most, a third stage lies in LDS instead of a second workgroup's (X X^T of six matrices of 1024 x 4096 in two parts, 216 tiles, 114 us, 139 by two;
+    // of 4096 x 8192, 528 tiles, 202 and 192).
     if (tiles[2] <= 256) launch_muon_tiles<2, 2, 3, MODE>(a, stream);
     else launch_muon_tiles<2, 2, 2, MODE>(a, stream);
   } else if (best == 3) {
