@@ -402,7 +402,7 @@ int zc_embedding(const void* d_table, int table_type, size_t table_rows, size_t 
 /* The table's gradient from that of the output, d_dy (n x cols): grad[v] = scale x the sum of dy[i] over all i with token[i] = v, zeros for a row that no token
  * names.  ZC_ADD: added to what d_grad holds; rows that no token names stay as they are.  Sums in binary32, rounded once; their order depends on the sizes and
  * the tokens only, so that equal calls give equal results.  d_ws: 16-byte aligned, its content irrelevant, one for calls that may overlap.
- * The tokens are read by table_rows / 1024 workgroups (256 at least), all of them by each. */
+ * d_grad does not overlap d_dy.  The tokens are read by table_rows / 1024 workgroups (256 at least), all of them by each. */
 size_t zc_embedding_workspace_bytes(size_t n, size_t table_rows, size_t cols);
 int zc_embedding_backward(const void* d_dy, int dy_type, size_t dy_stride, const void* d_tokens, int token_bits, size_t n, double scale, void* d_grad, int grad_type,
                           size_t table_rows, size_t cols, size_t grad_stride, unsigned flags, void* d_ws, size_t ws_bytes, void* hip_stream);
